@@ -55,7 +55,8 @@ typedef enum {
     DN_ERR_MODE = 4,       /* unknown nu_mode / bc mode, kl_modes outside 1..DN_MAX_KL_MODES */
     DN_ERR_WORKSPACE = 5,  /* workspace NULL, misaligned (256 B) or smaller than required  */
     DN_ERR_CUDA = 6,       /* a CUDA runtime call or kernel launch failed                  */
-    DN_ERR_ALIAS = 7       /* r overlaps u                                                 */
+    DN_ERR_ALIAS = 7,      /* an output overlaps an input (r and u, ...)                   */
+    DN_ERR_LAYOUT = 8      /* strides of dn_rows out of range, an array off its elements' alignment */
 } dn_status;
 
 typedef enum {
@@ -277,6 +278,76 @@ const char* dn_path_name(const dn_problem* problem);
 /* Name of the kernel that dn_energy_grad (r given) or dn_energy (r NULL) would run for these pointers, which are looked at for
  * their alignment only: "march2d", "tiled2d", "pair3d", "strip3d", "tiled3d" or "generic". */
 const char* dn_kernel_name(const dn_problem* problem, const float* u, const float* r);
+
+/* ---- What a generator uses next to the losses: a gated linear recurrence, activations, tensors saved in 8 bits -----------------
+ *
+ * Back-propagation (Algorithm 1) passes through the generator on its way from the loss to the weights, and the memory of its
+ * intermediate tensors is what bounds the size of the fields ("DiffNets": about 64 GB at 512^2 with 64 samples).  These entry points
+ * take fields in 32 or 16 bits; all arithmetic is in 32 bits, each result is rounded once. */
+typedef enum { DN_F32 = 0, DN_BF16 = 1, DN_F16 = 2 } dn_type;
+
+/* Values in 8 bits: blocks of 32 share a scale 2^e.  With A the largest finite magnitude of a block, 2^k <= A < 2^(k+1):
+ *   DN_INT8   e = max(k - 6, -126); integers -127 .. 127 times 2^e, the nearest (ties to even)
+ *   DN_E4M3   e = max(k - 7, -126); the nearest e4m3 number (3 bits of mantissa), at most 240, times 2^e
+ * A value that is not finite comes back as NaN and does not touch the others of its block. */
+typedef enum { DN_SAVE_FULL = 0, DN_INT8 = 1, DN_E4M3 = 2 } dn_format;
+
+/* An array [batch][rows][cols] of the type of the call, its columns adjacent; strides in elements.  Inputs: strides >= 0 (0: one
+ * row or sample read for all).  Outputs: no two elements in one place. */
+typedef struct {
+    void* data;
+    int64_t batch_stride, row_stride;
+} dn_rows;
+
+/* The recurrence, for every sample b and column c over the rows t (the time rows of a field [batch][nt][nx], say):
+ *
+ *   a_t = 1 / (1 + exp(-g_t)),   w_t = 1, or 1 - a_t with DN_SCAN_MIX
+ *   h_t = a_t h_{t-1} + w_t x_t,   t = 0 .. n_b - 1,   h_{-1} = h0 (0 where h0 is NULL)
+ *
+ * n_b = rows, or lengths[b] (values outside 0 .. rows count as the nearer of the two).  Rows from n_b on are not read; h, dg and dx
+ * are 0 there.  h_last[b] = h_{n_b - 1} (h0[b] if n_b = 0). */
+#define DN_SCAN_MIX 1u
+#define DN_SCAN_CHUNK 64         /* rows between two states that a checkpoint keeps in 32 bits */
+typedef struct {
+    int32_t batch, rows, cols;   /* batch, cols >= 1, rows >= 0                                             */
+    int32_t type;                /* dn_type of g, x, h and their gradients; h0, h_last are 32-bit floats [batch][cols] */
+    uint32_t flags;              /* DN_SCAN_MIX or 0                                                        */
+    int32_t format;              /* dn_format of gate and input in the checkpoint                           */
+    const int32_t* lengths;      /* [batch] on the device, or NULL                                          */
+} dn_scan;
+
+/* Bytes of the checkpoint that dn_scan_forward leaves for dn_scan_backward: the state ahead of every 64th row in 32 bits; with
+ * DN_INT8 or DN_E4M3 also gate and input in 8 bits, so that neither g nor x has to be kept (2.1 bytes per element in place of 4 or
+ * 8).  The gate is kept as DN_INT8 in either format: its error has to be small next to 1, not next to itself, or slow decays
+ * (1 - a = exp(-g) for large g) are lost.  0 if the call is invalid. */
+size_t dn_scan_checkpoint_bytes(const dn_scan* scan);
+
+/* h and h_last.  checkpoint (256-byte aligned, or NULL: nothing is kept) belongs to the caller, who hands it to the backward call.
+ * h_last may be NULL; it may be h0 itself (a step of a model that runs: rows = 1, the state updated in place). */
+dn_status dn_scan_forward(const dn_scan* scan, const dn_rows* g, const dn_rows* x, const float* h0, const dn_rows* h, float* h_last,
+                          void* checkpoint, size_t checkpoint_bytes, void* stream);
+
+/* The gradients of a loss with dh = dL/dh, dh_last = dL/dh_last (each may be NULL: 0), from the last row to the first:
+ *   l_t = dh_t + a_{t+1} l_{t+1} (+ dh_last at t = n_b - 1),   dx_t = w_t l_t,   dg_t = a_t (1 - a_t) l_t (h_{t-1} [- x_t with MIX]),
+ *   dh0 = a_0 l_0 (dh_last if n_b = 0; may be NULL).
+ * The states h are formed again from the checkpoint's.  With format DN_SAVE_FULL g and x are the forward call's; otherwise they are
+ * not looked at (NULL), and the result is these formulas at the values that the checkpoint holds. */
+dn_status dn_scan_backward(const dn_scan* scan, const dn_rows* g, const dn_rows* x, const void* checkpoint, size_t checkpoint_bytes,
+                           const dn_rows* dh, const float* dh_last, const dn_rows* dg, const dn_rows* dx, float* dh0, void* stream);
+
+/* n values in 8 bits, blocks of 32 as they lie in memory: dn_packed_bytes(n) bytes, 16-byte aligned. */
+size_t dn_packed_bytes(int64_t n);
+dn_status dn_pack(int64_t n, int32_t type, const void* src, int32_t format, void* packed, void* stream);
+dn_status dn_unpack(int64_t n, int32_t type, const void* packed, int32_t format, void* dst, void* stream);
+
+/* Pointwise activations whose backward pass needs only their input in 8 bits:
+ *   DN_SILU  y = x s(x);   DN_GELU  y = x s(2 z), z = sqrt(2/pi) (x + 0.044715 x^3) (the tanh form);   DN_TANH  y = tanh x
+ * with s(z) = 1 / (1 + exp(-z)).  The forward call writes y and the packed input, the backward call dx = dy f'(x) at the values that
+ * the packed input holds.  y must not overlap x; dx may be dy; packed may be NULL in the forward call (nothing is kept). */
+typedef enum { DN_SILU = 0, DN_GELU = 1, DN_TANH = 2 } dn_activation;
+dn_status dn_activation_forward(int64_t n, int32_t type, int32_t kind, const void* x, void* y, int32_t format, void* packed, void* stream);
+dn_status dn_activation_backward(int64_t n, int32_t type, int32_t kind, const void* packed, int32_t format, const void* dy, void* dx,
+                                 void* stream);
 
 const char* dn_status_string(dn_status status);
 

@@ -1,7 +1,13 @@
 """The physics loss as a differentiable PyTorch op: forward = per-sample energies J from the fused
 CUDA kernel, backward = the residual the same kernel produced (the loss gradient that enters the
-generator's back-propagation in Algorithm 1).  No autograd graph is built inside; there is no CPU path."""
+generator's back-propagation in Algorithm 1).  No autograd graph is built inside; there is no CPU path.
+
+Also two layers of a generator that the losses are back-propagated through: the gated recurrence over the time rows of
+a field, and pointwise activations, both able to keep what their backward pass needs in 8 bits (``checkpoints``
+does the same for the saved tensors of any other op, these losses' gradients among them)."""
 from __future__ import annotations
+
+from typing import Optional, Tuple
 
 import torch
 
@@ -65,3 +71,26 @@ def burgers_loss(u: torch.Tensor, problem: B.Burgers, workspace: torch.Tensor = 
     if workspace is None:
         workspace = B.new_burgers_workspace(problem)
     return _apply("burgers_loss", "dn_burgers_loss_grad", _BurgersLoss, u, problem, workspace)
+
+
+def gated_scan(gate: torch.Tensor, x: torch.Tensor, h0: Optional[torch.Tensor] = None, lengths: Optional[torch.Tensor] = None,
+               mix: bool = False, checkpoint: Optional[str] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """(h, h_last) of the recurrence h_t = a_t h_{t-1} + w_t x_t over the rows of fields [batch, rows, cols], a = sigmoid(gate),
+    w = 1 or, with ``mix``, 1 - a; h0 and h_last: [batch, cols] float32; lengths: [batch] int32, rows behind them are 0.
+    gate and x: CUDA tensors of one type (float32, bfloat16, float16).  Differentiable once, with respect to gate, x and h0.
+
+    checkpoint None keeps gate, x and the state ahead of every 64th row for the backward pass; "int8" or "e4m3" keeps gate and x
+    in 8 bits instead (the gate as int8 in either), and the gradients are those at the values that 8 bits hold."""
+    out = B.native().gated_scan(gate, x, h0, lengths, mix, B._format(checkpoint, none=True))
+    if isinstance(out, int):
+        raise B.DnError(out, "dn_scan_forward")
+    return out
+
+
+def activation(x: torch.Tensor, kind: str = "silu", checkpoint: str = "int8") -> torch.Tensor:
+    """"silu", "gelu" (its tanh form) or "tanh" of a CUDA tensor, which keeps its input for the backward pass in 8 bits ("int8" or
+    "e4m3"): the gradient is dy f'(x) at the values that 8 bits hold.  Differentiable once."""
+    y = B.native().activation(x, B._kind(kind), B._format(checkpoint))
+    if isinstance(y, int):
+        raise B.DnError(y, "dn_activation_forward")
+    return y

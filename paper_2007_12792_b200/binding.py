@@ -19,7 +19,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libdn.so")
 
 DN_OK = 0
-DN_ERR_NULL, DN_ERR_DIM, DN_ERR_SIZE, DN_ERR_MODE, DN_ERR_WORKSPACE, DN_ERR_CUDA, DN_ERR_ALIAS = range(1, 8)
+DN_ERR_NULL, DN_ERR_DIM, DN_ERR_SIZE, DN_ERR_MODE, DN_ERR_WORKSPACE, DN_ERR_CUDA, DN_ERR_ALIAS, DN_ERR_LAYOUT = range(1, 9)
 DN_NU_NODAL = 0
 DN_NU_KL_GAUSS = 1
 DN_NU_KL_NODAL = 2
@@ -27,11 +27,20 @@ DN_IMPOSE_BC_ON_LOAD = 1
 DN_NO_MASK = 2
 DN_FORCE_GENERIC = 4
 DN_MAX_KL_MODES = 8
+DN_F32, DN_BF16, DN_F16 = range(3)
+DN_SAVE_FULL, DN_INT8, DN_E4M3 = range(3)
+DN_SILU, DN_GELU, DN_TANH = range(3)
+DN_SCAN_MIX = 1
+DN_SCAN_CHUNK = 64
+FORMATS = {None: DN_SAVE_FULL, "int8": DN_INT8, "e4m3": DN_E4M3}
+ACTIVATIONS = {"silu": DN_SILU, "gelu": DN_GELU, "tanh": DN_TANH}
 
 EXPORTS = ("dn_apply_bc_per_sample", "dn_workspace_bytes", "dn_host_staging_bytes", "dn_kl_field", "dn_energy", "dn_energy_grad",
            "dn_apply_bc", "dn_energy_grad_host", "dn_energy_grad_traced", "dn_energy_grad_static", "dn_launches_per_call", "dn_path_name", "dn_kernel_name", "dn_status_string",
            "dn_burgers_workspace_bytes", "dn_burgers_loss_grad", "dn_burgers_path_name",
-           "dn_burgers_host_staging_bytes", "dn_burgers_loss_grad_host", "dn_cg_workspace_bytes", "dn_cg_solve")
+           "dn_burgers_host_staging_bytes", "dn_burgers_loss_grad_host", "dn_cg_workspace_bytes", "dn_cg_solve",
+           "dn_scan_checkpoint_bytes", "dn_scan_forward", "dn_scan_backward", "dn_packed_bytes", "dn_pack", "dn_unpack",
+           "dn_activation_forward", "dn_activation_backward")
 
 
 class DnGrid(C.Structure):
@@ -50,6 +59,15 @@ class DnProblem(C.Structure):
 class DnBurgers(C.Structure):
     _fields_ = [("nx", C.c_int32), ("nt", C.c_int32), ("batch", C.c_int32), ("T", C.c_float), ("lam", C.c_float),
                 ("c", C.c_void_p), ("flags", C.c_uint32)]
+
+
+class DnRows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("batch_stride", C.c_int64), ("row_stride", C.c_int64)]
+
+
+class DnScan(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("rows", C.c_int32), ("cols", C.c_int32), ("type", C.c_int32), ("flags", C.c_uint32),
+                ("format", C.c_int32), ("lengths", C.c_void_p)]
 
 
 class DnError(RuntimeError):
@@ -102,6 +120,19 @@ def lib():
                                                 C.c_size_t, C.c_void_p]
         L.dn_burgers_loss_grad_host.restype = C.c_int
         L.dn_burgers_path_name.argtypes = [PB, C.c_void_p, C.c_void_p]; L.dn_burgers_path_name.restype = C.c_char_p
+        PS, PR = C.POINTER(DnScan), C.POINTER(DnRows)
+        L.dn_scan_checkpoint_bytes.argtypes = [PS]; L.dn_scan_checkpoint_bytes.restype = C.c_size_t
+        L.dn_scan_forward.argtypes = [PS, PR, PR, C.c_void_p, PR, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+        L.dn_scan_forward.restype = C.c_int
+        L.dn_scan_backward.argtypes = [PS, PR, PR, C.c_void_p, C.c_size_t, PR, C.c_void_p, PR, PR, C.c_void_p, C.c_void_p]
+        L.dn_scan_backward.restype = C.c_int
+        L.dn_packed_bytes.argtypes = [C.c_int64]; L.dn_packed_bytes.restype = C.c_size_t
+        L.dn_pack.argtypes = [C.c_int64, C.c_int32, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p]; L.dn_pack.restype = C.c_int
+        L.dn_unpack.argtypes = [C.c_int64, C.c_int32, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p]; L.dn_unpack.restype = C.c_int
+        L.dn_activation_forward.argtypes = [C.c_int64, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p]
+        L.dn_activation_forward.restype = C.c_int
+        L.dn_activation_backward.argtypes = [C.c_int64, C.c_int32, C.c_int32, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p]
+        L.dn_activation_backward.restype = C.c_int
         for f in ("dn_kl_field", "dn_energy", "dn_energy_grad", "dn_apply_bc", "dn_energy_grad_host", "dn_energy_grad_traced"):
             getattr(L, f).restype = C.c_int
         _lib = L
@@ -404,3 +435,91 @@ def dn_cg_solve(problem: Problem, u: torch.Tensor, max_iters: int, rtol: float, 
                              None if iters is None else iters.data_ptr(), workspace.data_ptr(), workspace.numel(),
                              _stream(stream)), "dn_cg_solve")
     return u
+
+
+# ---- what a generator uses next to the losses: the gated recurrence, activations and tensors saved in 8 bits ----------------
+def _format(name, none=False) -> int:
+    if name not in FORMATS or (name is None and not none):
+        raise ValueError(f"format: expected {'None, ' if none else ''}'int8' or 'e4m3', found {name!r}")
+    return FORMATS[name]
+
+
+def _kind(name) -> int:
+    if name not in ACTIVATIONS:
+        raise ValueError(f"kind: expected 'silu', 'gelu' or 'tanh', found {name!r}")
+    return ACTIVATIONS[name]
+
+
+@dataclass
+class Scan:
+    """Python mirror of ``dn_scan``: the gated recurrence over the rows of fields [batch][rows][cols]."""
+    batch: int
+    rows: int
+    cols: int
+    dtype: torch.dtype = torch.float32         # of the gate, the input, h and their gradients
+    mix: bool = False                          # w_t = 1 - a_t in place of 1
+    checkpoint: Optional[str] = None           # gate and input in the checkpoint: None (not kept there), "int8" or "e4m3"
+    lengths: Optional[torch.Tensor] = None     # [batch] int32 on the device
+
+    def __post_init__(self):
+        self.format = _format(self.checkpoint, none=True)
+
+    @property
+    def shape(self):
+        return (self.batch, self.rows, self.cols)
+
+
+def dn_scan_checkpoint_bytes(problem: Scan) -> int:
+    return int((_native or native()).scan_checkpoint_bytes(problem))
+
+
+def new_scan_checkpoint(problem: Scan, device="cuda") -> torch.Tensor:
+    return torch.empty(max(dn_scan_checkpoint_bytes(problem), 256), dtype=torch.uint8, device=device)
+
+
+def dn_scan_forward(problem: Scan, g: torch.Tensor, x: torch.Tensor, h0: Optional[torch.Tensor], h: torch.Tensor,
+                    h_last: Optional[torch.Tensor], checkpoint: Optional[torch.Tensor] = None, stream=None):
+    """h and h_last of the recurrence; g, x, h: [batch, rows, cols] with adjacent columns, h0 and h_last: [batch, cols] float32.
+    h_last may be h0.  checkpoint (new_scan_checkpoint) is for dn_scan_backward; None keeps nothing."""
+    _check((_native or native()).scan_forward(problem, g, x, h0, h, h_last, checkpoint, None if stream is None else _stream(stream)),
+           "dn_scan_forward")
+    return h, h_last
+
+
+def dn_scan_backward(problem: Scan, g: Optional[torch.Tensor], x: Optional[torch.Tensor], checkpoint: torch.Tensor,
+                     dh: Optional[torch.Tensor], dh_last: Optional[torch.Tensor], dg: torch.Tensor, dx: torch.Tensor,
+                     dh0: Optional[torch.Tensor], stream=None):
+    """The gradients dg, dx, dh0 from dh and dh_last (either may be None).  With problem.checkpoint set, g and x are not looked at."""
+    _check((_native or native()).scan_backward(problem, g, x, checkpoint, dh, dh_last, dg, dx, dh0,
+                                               None if stream is None else _stream(stream)), "dn_scan_backward")
+    return dg, dx, dh0
+
+
+def dn_packed_bytes(n: int) -> int:
+    return int(lib().dn_packed_bytes(int(n)))
+
+
+def dn_pack(src: torch.Tensor, format: str, packed: torch.Tensor, stream=None) -> torch.Tensor:
+    """The values of src (contiguous) in 8 bits: packed is a uint8 tensor of dn_packed_bytes(src.numel()) bytes."""
+    _check((_native or native()).pack(src, _format(format), packed, None if stream is None else _stream(stream)), "dn_pack")
+    return packed
+
+
+def dn_unpack(packed: torch.Tensor, format: str, dst: torch.Tensor, stream=None) -> torch.Tensor:
+    _check((_native or native()).unpack(packed, _format(format), dst, None if stream is None else _stream(stream)), "dn_unpack")
+    return dst
+
+
+def dn_activation_forward(kind: str, x: torch.Tensor, y: torch.Tensor, format: str = "int8", packed: Optional[torch.Tensor] = None,
+                          stream=None):
+    """y = f(x) for kind "silu", "gelu" (tanh form) or "tanh"; packed (None: nothing is kept) receives x in 8 bits."""
+    _check((_native or native()).activation_forward(_kind(kind), x, y, _format(format), packed, None if stream is None else _stream(stream)),
+           "dn_activation_forward")
+    return y, packed
+
+
+def dn_activation_backward(kind: str, packed: torch.Tensor, format: str, dy: torch.Tensor, dx: torch.Tensor, stream=None):
+    """dx = dy f'(x) at the values that packed holds; dx may be dy."""
+    _check((_native or native()).activation_backward(_kind(kind), packed, _format(format), dy, dx, None if stream is None else _stream(stream)),
+           "dn_activation_backward")
+    return dx

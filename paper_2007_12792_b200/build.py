@@ -18,10 +18,11 @@ NATIVE = os.path.join(HERE, "_native.so")      # native marshalling for Python (
 SOURCES = [(f, f.replace(".cu", ".o"), []) for f in
            ["dn_api.cu", "dn_aux.cu", "dn_generic.cu", "dn_tiled2d.cu", "dn_march2d.cu", "dn_tiled3d.cu",
             "dn_pair3d.cu", "dn_strip3d.cu", "dn_static.cu", "dn_burgers.cu", "dn_cg.cu",
-            "dn_multigrid.cu"]]
+            "dn_multigrid.cu", "dn_scan.cu", "dn_saved.cu"]]
 SOURCES += [("dn_march2d.cu", f"dn_march2d_{k}.o", [f"-DDN_M2_PART={k}"]) for k in (1, 2, 3)]
 SOURCES += [("dn_pair3d.cu", f"dn_pair3d_{k}.o", [f"-DDN_P3_PART={k}"]) for k in (1, 2, 3)]
 HEADERS = [os.path.join(CSRC, "dn_internal.cuh"), os.path.join(ROOT, "include", "dn.h")]
+EIGHT = {"dn_scan.cu", "dn_saved.cu"}          # these also include dn_eight.cuh
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-I" + os.path.join(ROOT, "include"), "-I" + CSRC]
 
@@ -55,7 +56,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
         path = os.path.join(CSRC, src)
         obj = os.path.join(objdir, objname)
         objs.append(obj)
-        if force or _stale(obj, [path] + HEADERS):
+        if force or _stale(obj, [path] + HEADERS + ([os.path.join(CSRC, "dn_eight.cuh")] if src in EIGHT else [])):
             cmd = [nvcc] + NVCC_FLAGS + extra + (["-Xptxas", "-v"] if verbose else []) + ["-c", path, "-o", obj]
             procs.append((objname, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
     failed = False

@@ -1,0 +1,67 @@
+"""Saved tensors in 8 bits: what a training step keeps between forward and backward pass, in a quarter (float32) or half of its bytes.
+
+``pack`` puts one tensor into 8 bits, ``saved_in_8_bits`` does so with what the ops inside it save for their backward pass: a
+generator's layers, and the gradient that the losses of ``autograd`` compute with their value.  Blocks of 32 values share a scale
+that is a power of two ("int8": errors of at most 1/128 of the block's largest magnitude, "e4m3": of 1/16 of the value itself);
+a value that is not finite comes back as NaN."""
+from __future__ import annotations
+
+from dataclasses import dataclass
+from typing import Iterable
+
+import torch
+
+from . import binding as B
+
+TYPES = (torch.float32, torch.bfloat16, torch.float16)
+
+
+@dataclass
+class Packed:
+    """A tensor in 8 bits."""
+    data: torch.Tensor           # uint8: the codes, then a byte per block of 32 for its scale
+    format: str
+    shape: torch.Size
+    dtype: torch.dtype
+
+    def unpack(self) -> torch.Tensor:
+        """The values that stand for the tensor: contiguous, of its type, on its device."""
+        out = torch.empty(self.shape, dtype=self.dtype, device=self.data.device)
+        if out.numel():
+            B.dn_unpack(self.data, self.format, out)
+        return out
+
+
+def pack(x: torch.Tensor, format: str = "int8") -> Packed:
+    """x (CUDA, float32, bfloat16 or float16, any shape and strides) in 8 bits, in blocks of 32 along its elements in order."""
+    B._format(format)
+    x = x.detach().contiguous()
+    data = torch.empty(max(B.dn_packed_bytes(x.numel()), 1), dtype=torch.uint8, device=x.device)
+    if x.numel():
+        B.dn_pack(x, format, data)
+    return Packed(data, format, x.shape, x.dtype)
+
+
+class saved_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
+    """Context in which the floating-point CUDA tensors that autograd saves are kept in 8 bits:
+
+        with saved_in_8_bits(keep=generator.parameters()):
+            loss = energy(generator(z), problem).mean()
+        loss.backward()
+
+    keep: tensors that stay as they are, views of them too (weights, which the gradient of the input multiplies with); so do
+    tensors of less than ``min_numel`` elements.  A gradient is then that of the ops at the values which 8 bits hold."""
+
+    def __init__(self, format: str = "int8", keep: Iterable[torch.Tensor] = (), min_numel: int = 4096):
+        B._format(format)
+        keep = tuple(keep)                                     # held: an address stands for its tensor only while that lives
+
+        def put(t):
+            if not t.is_cuda or t.dtype not in TYPES or t.numel() < min_numel:
+                return t
+            place = t.untyped_storage().data_ptr()
+            if any(k.is_cuda and k.untyped_storage().data_ptr() == place for k in keep):
+                return t
+            return pack(t, format)
+
+        super().__init__(put, lambda p: p.unpack() if isinstance(p, Packed) else p)

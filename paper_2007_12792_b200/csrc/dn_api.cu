@@ -549,7 +549,8 @@ const char* dn_status_string(dn_status s) {
         case DN_ERR_MODE: return "unknown mode or kl_modes out of range";
         case DN_ERR_WORKSPACE: return "workspace missing, misaligned or too small";
         case DN_ERR_CUDA: return "CUDA runtime error";
-        case DN_ERR_ALIAS: return "r overlaps u";
+        case DN_ERR_ALIAS: return "an output overlaps an input";
+        case DN_ERR_LAYOUT: return "strides out of range or an array off its alignment";
     }
     return "unknown status";
 }
