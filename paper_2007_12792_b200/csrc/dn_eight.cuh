@@ -55,13 +55,49 @@ template <> __device__ __forceinline__ float rounded<float>(float v) { return v;
 template <> __device__ __forceinline__ __nv_bfloat16 rounded<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 template <> __device__ __forceinline__ __half rounded<__half>(float v) { return __float2half_rn(v); }
 
-// p = 1 / (1 + e^-z) and q = 1 / (1 + e^z).  The smaller is e^-|z| / (1 + e^-|z|), to a few units in its own last place (one minus the
-// other would have 10 bits left for z = 10); the larger is one minus the smaller, which is rounded once: a quotient would be off by a few
-// units of 2^-24, the same way row after row, and a decay near 1 multiplies hundreds of them.  e^-|z| cannot overflow, and both are
-// exactly 0 or 1 at z = +-inf.  ACCURATE: expf instead of the approximate exponential, whose
-// relative error grows with |z| to 1e-6; 16-bit results do not show that.
-template <bool ACCURATE>
-__device__ __forceinline__ void gates(float z, float& p, float& q) {
+// Values of V adjacent columns; two are worked on by one instruction where there is one for pairs.
+template <int V> struct __align__(4 * V) Cols { float v[V]; };
+template <int V> __device__ __forceinline__ Cols<V> all_of(float f) {
+    Cols<V> r;
+#pragma unroll
+    for (int v = 0; v < V; ++v) r.v[v] = f;
+    return r;
+}
+__device__ __forceinline__ unsigned long long pair_bits(const Cols<2>& c) {
+    unsigned long long r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(c.v[0]), "f"(c.v[1]));
+    return r;
+}
+__device__ __forceinline__ Cols<2> pair_of(unsigned long long b) {
+    Cols<2> r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.v[0]), "=f"(r.v[1]) : "l"(b));
+    return r;
+}
+__device__ __forceinline__ Cols<1> mul(Cols<1> a, Cols<1> b) { return Cols<1>{{a.v[0] * b.v[0]}}; }
+__device__ __forceinline__ Cols<1> add(Cols<1> a, Cols<1> b) { return Cols<1>{{a.v[0] + b.v[0]}}; }
+__device__ __forceinline__ Cols<1> fma(Cols<1> a, Cols<1> b, Cols<1> c) { return Cols<1>{{fmaf(a.v[0], b.v[0], c.v[0])}}; }
+__device__ __forceinline__ Cols<2> mul(Cols<2> a, Cols<2> b) {
+    unsigned long long r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(pair_bits(a)), "l"(pair_bits(b)));
+    return pair_of(r);
+}
+__device__ __forceinline__ Cols<2> add(Cols<2> a, Cols<2> b) {
+    unsigned long long r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(pair_bits(a)), "l"(pair_bits(b)));
+    return pair_of(r);
+}
+__device__ __forceinline__ Cols<2> fma(Cols<2> a, Cols<2> b, Cols<2> c) {
+    unsigned long long r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(pair_bits(a)), "l"(pair_bits(b)), "l"(pair_bits(c)));
+    return pair_of(r);
+}
+
+// p = 1 / (1 + e^-z) and q = 1 / (1 + e^z), each to a few units in its own last place (one minus the other would have 10 bits left for
+// z = 10): the smaller is e^-|z| / (1 + e^-|z|), the larger is one minus the smaller, which is rounded once: a quotient would be off by a
+// unit of 2^-24, the same way row after row, and a decay near 1 multiplies hundreds of them.  Both are exactly 0 or 1 at z = +-inf.
+// ACCURATE, for 32-bit results: expf; else the approximate exponential, whose relative error grows with |z| to 1e-6, which 16-bit
+// results do not show.
+template <bool ACCURATE> __device__ __forceinline__ void two_sided_gates(float z, float& p, float& q) {
     const float e = ACCURATE ? expf(-fabsf(z)) : __expf(-fabsf(z));
     const float less = __fdividef(e, 1.0f + e), more = 1.0f - less;
     const bool up = z >= 0.0f;
@@ -69,6 +105,38 @@ __device__ __forceinline__ void gates(float z, float& p, float& q) {
     q = up ? less : more;
 }
 
+// The same as the decay and the input's weight of the recurrence.  For 16-bit types with z held to at least LEAST_GATE, so that e^-z cannot
+// overflow, and what that leaves of p (2^-125) taken away, so that p is 0 there: 6 operations instead of some 16, 10 for two columns.
+// HELD: the caller has held z.  none: least_decay().
+constexpr float LEAST_GATE = -87.0f;
+__device__ __forceinline__ void exponential_gate(float t, float& e) { asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(t)); }
+__device__ __forceinline__ void reciprocal_gate(float d, float& p) { asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(p) : "f"(d)); }
+__device__ __forceinline__ float least_decay() {           // the operations of gates() below, at LEAST_GATE
+    float e, p;
+    exponential_gate(__fmul_rn(LEAST_GATE, -1.4426950408889634f), e);
+    reciprocal_gate(__fadd_rn(e, 1.0f), p);
+    return -p;
+}
+template <bool ACCURATE, bool HELD = false, int V>
+__device__ __forceinline__ void gates(const Cols<V>& z, Cols<V>& p, Cols<V>& q, float none) {
+    if constexpr (ACCURATE) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) two_sided_gates<true>(z.v[v], p.v[v], q.v[v]);
+    } else {
+        Cols<V> t = z, e;
+        if (!HELD)
+#pragma unroll
+            for (int v = 0; v < V; ++v) asm("max.NaN.f32 %0, %0, %1;" : "+f"(t.v[v]) : "f"(LEAST_GATE));
+        t = mul(t, all_of<V>(-1.4426950408889634f));       // - log2 e
+#pragma unroll
+        for (int v = 0; v < V; ++v) exponential_gate(t.v[v], e.v[v]);
+        const Cols<V> d = add(e, all_of<V>(1.0f));
+#pragma unroll
+        for (int v = 0; v < V; ++v) reciprocal_gate(d.v[v], p.v[v]);
+        q = mul(e, p);
+        p = add(p, all_of<V>(none));
+    }
+}
 // |v| as bits, 0 where v is not finite: the order of these as integers is that of the magnitudes
 __device__ __forceinline__ unsigned magnitude_bits(float v) {
     const unsigned m = __float_as_uint(v) & 0x7fffffffu;
@@ -101,6 +169,40 @@ __device__ __forceinline__ float value_e4m3(unsigned code, float scale) {
     return __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)code, __NV_E4M3))) * scale;
 }
 __device__ __forceinline__ float value8(unsigned code, float scale, bool int8) { return int8 ? value_int8(code, scale) : value_e4m3(code, scale); }
+
+// Codes of V adjacent columns, first column in the lowest byte.  v / 2^e + 2^23 + 2^22 + 128 is rounded to an integer by the sum itself
+// (the quotient is exact, and inside a fused product and sum not even formed); the code then stands in the last bits.  The values are
+// finite.
+__device__ __forceinline__ uint32_t codes_int8(const Cols<1>& v, float inverse) {
+    const int t = __float_as_int(fmaf(v.v[0], inverse, 12583040.0f));
+    return (uint32_t)(min(max(t, 0x4b400001), 0x4b4000ff) & 255);
+}
+__device__ __forceinline__ uint32_t codes_int8(const Cols<2>& v, float inverse) {
+    const Cols<2> t = fma(v, all_of<2>(inverse), all_of<2>(12583040.0f));
+    const uint32_t w = __byte_perm(__float_as_uint(t.v[0]), __float_as_uint(t.v[1]), 0x5410);      // 0 .. 256 in either half
+    return __byte_perm(__vmaxu2(__vminu2(w, 0x00ff00ffu), 0x00010001u), 0u, 0x4420);
+}
+__device__ __forceinline__ uint32_t codes_e4m3(const Cols<1>& v, float inverse) { return code_e4m3(v.v[0], inverse); }
+__device__ __forceinline__ uint32_t codes_e4m3(const Cols<2>& v, float inverse) {
+    const Cols<2> t = mul(v, all_of<2>(inverse));
+    const float2 h = make_float2(fminf(fmaxf(t.v[0], -240.0f), 240.0f), fminf(fmaxf(t.v[1], -240.0f), 240.0f));
+    return (uint32_t)__nv_cvt_float2_to_fp8x2(h, __NV_SATFINITE, __NV_E4M3);
+}
+// ... and back.  A code 0, not a number, is read as -128 here: the caller looks for it (any_zero_byte).
+template <int V> __device__ __forceinline__ Cols<V> values_int8(uint32_t codes, float scale) {
+    Cols<V> f;
+    f.v[0] = __uint_as_float(__byte_perm(codes, 0x4b000000u, 0x7440));
+    if constexpr (V == 2) f.v[1] = __uint_as_float(__byte_perm(codes, 0x4b000000u, 0x7441));
+    return mul(add(f, all_of<V>(-8388736.0f)), all_of<V>(scale));
+}
+template <int V> __device__ __forceinline__ Cols<V> values_e4m3(uint32_t codes, float scale) {
+    if constexpr (V == 1) return Cols<1>{{value_e4m3(codes, scale)}};
+    else {
+        const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)codes, __NV_E4M3);
+        return mul(Cols<2>{{__half2float(__half(__half_raw{h.x})), __half2float(__half(__half_raw{h.y}))}}, all_of<2>(scale));
+    }
+}
+__device__ __forceinline__ uint32_t any_zero_byte(uint32_t w) { return (w - 0x01010101u) & ~w & 0x80808080u; }
 #endif
 
 }  // namespace dn

@@ -98,17 +98,17 @@ template <int KIND> __device__ __forceinline__ float gate_argument(float x, floa
 template <int KIND, bool ACCURATE> __device__ __forceinline__ float activation(float x) {
     if (KIND == DN_TANH) return tanhf(x);
     float dz, p, q;
-    gates<ACCURATE>(gate_argument<KIND>(x, dz), p, q);
+    two_sided_gates<ACCURATE>(gate_argument<KIND>(x, dz), p, q);
     return x * p;
 }
 template <int KIND, bool ACCURATE> __device__ __forceinline__ float slope(float x) {
     float dz, p, q;
     if (KIND == DN_TANH) {                                 // 1 - tanh^2 = 4 s(2x) s(-2x), which keeps its digits where tanh is near 1
-        gates<ACCURATE>(2.0f * x, p, q);
+        two_sided_gates<ACCURATE>(2.0f * x, p, q);
         return 4.0f * p * q;
     }
     const float z = gate_argument<KIND>(x, dz);
-    gates<ACCURATE>(z, p, q);
+    two_sided_gates<ACCURATE>(z, p, q);
     if (KIND == DN_GELU) x = fabsf(x) > 16.0f ? copysignf(16.0f, x) : x;
     return p * fmaf(x * q, dz, 1.0f);
 }

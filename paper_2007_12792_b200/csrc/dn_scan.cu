@@ -29,30 +29,40 @@ struct ScanArgs {
     float* states;
     int64_t rows_padded;
     int rows, cols, strips, blocks, nblk, nchunk;
-    int mix, int8;               // int8: the input's format (the gate's always is)
+    int int8;                    // the input's format (the gate's always is)
 };
 
 template <class T, int V> using Raw = std::conditional_t<sizeof(T) * V == 4, uint32_t, uint16_t>;
 
-template <class T, int V> __device__ __forceinline__ void expand(Raw<T, V> r, float (&f)[V]) {
-    if constexpr (V == 1) {
-        T t;
-        memcpy(&t, &r, sizeof t);
-        f[0] = as_float(t);
-    } else {
-        T t[2];
-        memcpy(t, &r, sizeof t);
-        f[0] = as_float(t[0]);
-        f[1] = as_float(t[1]);
-    }
+template <class T, int V> __device__ __forceinline__ Cols<V> expand(Raw<T, V> r) {
+    T t[V];
+    memcpy(t, &r, sizeof t);
+    Cols<V> f;
+#pragma unroll
+    for (int v = 0; v < V; ++v) f.v[v] = as_float(t[v]);
+    return f;
 }
-template <class T, int V> __device__ __forceinline__ Raw<T, V> join(const float (&f)[V]) {
+template <class T, int V> __device__ __forceinline__ Raw<T, V> join(const Cols<V>& f) {
     T t[V];
 #pragma unroll
-    for (int v = 0; v < V; ++v) t[v] = rounded<T>(f[v]);
+    for (int v = 0; v < V; ++v) t[v] = rounded<T>(f.v[v]);
     Raw<T, V> r;
     memcpy(&r, t, sizeof r);
     return r;
+}
+// gates of 16-bit values are held to LEAST_GATE in 16 bits, both columns at once (-87 is a value of both types)
+__device__ __forceinline__ uint32_t held(uint32_t r, __nv_bfloat16) {
+    asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(r) : "r"(0xc2aec2aeu));
+    return r;
+}
+__device__ __forceinline__ uint32_t held(uint32_t r, __half) {
+    asm("max.NaN.f16x2 %0, %0, %1;" : "+r"(r) : "r"(0xd570d570u));
+    return r;
+}
+template <class T, int V> __device__ __forceinline__ void gate_parts(Raw<T, V> r, Cols<V>& a, Cols<V>& w, float none) {
+    if constexpr (sizeof(T) == 4) gates<true>(expand<T, V>(r), a, w, none);
+    else if constexpr (V == 2) gates<false, true>(expand<T, V>(held(r, T())), a, w, none);
+    else gates<false>(expand<T, V>(r), a, w, none);
 }
 template <class W> __device__ __forceinline__ W load_at(const char* p) { return *reinterpret_cast<const W*>(p); }
 template <class W> __device__ __forceinline__ void store_at(char* p, W v) { *reinterpret_cast<W*>(p) = v; }
@@ -62,16 +72,44 @@ __device__ __forceinline__ unsigned cluster_address(const void* local, int rank)
     asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"((unsigned)__cvta_generic_to_shared(local)), "r"(rank));
     return r;
 }
-__device__ __forceinline__ void cluster_store(unsigned at, float v) { asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at), "f"(v) : "memory"); }
-__device__ __forceinline__ void cluster_barrier() {
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+// A store into a block of the cluster that counts its bytes at a barrier there: what waits at the barrier sees what was stored.  A barrier
+// of the whole cluster would make each block wait for its own stores of h as well.
+__device__ __forceinline__ void cluster_send(unsigned at, unsigned bar, float a, float b) {
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];" ::"r"(at), "f"(a), "f"(b), "r"(bar) : "memory");
 }
+__device__ __forceinline__ void cluster_send(unsigned at, unsigned bar, float a, float b, float c, float d) {
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(at), "f"(a), "f"(b), "f"(c), "f"(d), "r"(bar)
+                 : "memory");
+}
+__device__ __forceinline__ void barrier_init(uint64_t* bar) { asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"((unsigned)__cvta_generic_to_shared(bar)) : "memory"); }
+__device__ __forceinline__ void barrier_expect(uint64_t* bar, unsigned bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"((unsigned)__cvta_generic_to_shared(bar)), "r"(bytes) : "memory");
+}
+// The blocks of a cluster run together, so the wait ends; should it ever not (2^20 tries, each of which suspends the thread for a while),
+// false: the caller's results become NaN.
+__device__ __forceinline__ bool barrier_wait(uint64_t* bar, unsigned parity) {
+    const unsigned at = (unsigned)__cvta_generic_to_shared(bar);
+    for (int i = 0; i < 1 << 20; ++i) {
+        unsigned done;
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                     : "=r"(done) : "r"(at), "r"(parity) : "memory");
+        if (done) return true;
+    }
+    return false;
+}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
-// Where a thread works: lanes LX across the columns (V each) and 32 / LX down the rows, warps WR down and WC across.
+// factors and offsets of V adjacent columns, in one access
+template <int V> struct __align__(8 * V) Maps { Cols<V> p, h; };
+
+// Where a thread works: lanes LX across the columns (V each) and 32 / LX down the rows, warps WR down and WC across, R rows each.
+// An address is a place that is the same for the whole block, which the uniform registers hold, plus the thread's own offset, which does
+// not change; Off is 64 bits wide only for rows so far apart that a tile of them passes 4 GiB.
 template <int V, int LX, int WR, int WC, int R> struct Place {
     static constexpr int NG = WR * (32 / LX), COLS = WC * LX * V, TILE = NG * R, THREADS = 32 * WR * WC;
-    int b, rank, q, col, c, len;
-    bool cv;
+    int b, rank, first, q, col, c, len;
+    bool cv, all;                // this thread's columns exist; the block's do
     __device__ Place(const ScanArgs& A) {
         const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
         q = (warp % WR) * (32 / LX) + lane / LX;
@@ -79,381 +117,446 @@ template <int V, int LX, int WR, int WC, int R> struct Place {
         const unsigned unit = blockIdx.x / A.blocks;
         rank = blockIdx.x % A.blocks;
         b = unit / A.strips;
-        c = (int)(unit % A.strips) * COLS + col;
+        first = (int)(unit % A.strips) * COLS;
+        c = first + col;
         cv = c < A.cols;
+        all = first + COLS <= A.cols;
         len = A.rows;
     }
     __device__ void read_length(const ScanArgs& A) {
         if (A.lengths) len = min(max(A.lengths[b], 0), A.rows);
     }
+    __device__ char* base(const RowsOf& r, int size) const { return r.p + b * r.batch + first * (int64_t)size; }
+    template <class Off> __device__ Off offset(const RowsOf& r, int size) const { return (Off)(q * R) * (Off)r.row + (Off)(col * size); }
+};
+using Yes = std::true_type;
+using No = std::false_type;
+
+// Magnitudes of a row's gate (low half) and input (high half), the larger of the thread's columns: the upper 16 bits without the sign, whose
+// order as integers is that of the magnitudes.
+template <class T, int V> __device__ __forceinline__ uint32_t magnitudes(Raw<T, V> g, Raw<T, V> x) {
+    if constexpr (sizeof(T) == 4) return __byte_perm(g, x, 0x7632) & 0x7fff7fffu;
+    else if constexpr (V == 1) return (g | (uint32_t)x << 16) & 0x7fff7fffu;
+    else return __vmaxu2(__byte_perm(g, x, 0x5410) & 0x7fff7fffu, __byte_perm(g, x, 0x7632) & 0x7fff7fffu);
+}
+template <class T> __device__ __forceinline__ int exponent_of(uint32_t magnitude) {          // biased; 255: not finite
+    if constexpr (std::is_same_v<T, __half>) return (int)(__float_as_uint(__half2float(__ushort_as_half((unsigned short)magnitude))) >> 23);
+    else return (int)(magnitude >> 7);
+}
+
+// Per block: where it stands, and what a step of it exchanges.  The blocks of a cluster send one another the map of their tile; a buffer
+// is written again two steps later, when its readers have sent what they found with it.
+template <int V, int LX, int WR, int WC, int R> struct Exchange {
+    using Pl = Place<V, LX, WR, WC, R>;
+    static constexpr int NG = Pl::NG, LANES = WC * LX;
+    Maps<V> agg[2][NG > 1 ? NG : 1][NG > 1 ? LANES : 1];
+    Maps<V> tot[2][SCAN_MOST_BLOCKS][NG > 1 ? LANES : 1];
+    uint64_t bars[2];
+
+    __device__ void init(int K) {
+        if (K > 1 && threadIdx.x == 0) {
+            barrier_init(&bars[0]);
+            barrier_init(&bars[1]);
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        }
+    }
+    // The value that enters this thread's rows, from the map (p, h) of these rows and the value `carry` that enters the step's first ones;
+    // carry becomes what leaves the last ones.  DOWN: rows are passed from the last to the first.  `between`: what to do once all maps of
+    // the block can be read.
+    template <bool DOWN, class F> __device__ __forceinline__ Cols<V> enter(int k, int K, int rank, int q, int lane, const Cols<V>& p, const Cols<V>& h, Cols<V>& carry, bool& lost, F between) {
+        if constexpr (NG == 1) {
+            const Cols<V> in = carry;
+            carry = fma(p, carry, h);
+            between();
+            return in;
+        } else {
+            const int buf = k & 1;
+            agg[buf][q][lane] = Maps<V>{p, h};
+            __syncthreads();
+            between();
+            Cols<V> in = carry;
+            if (K == 1) {
+#pragma unroll
+                for (int i = 0; i < NG; ++i) {
+                    const int j = DOWN ? NG - 1 - i : i;
+                    const Maps<V> e = agg[buf][j][lane];
+                    if (j == q) in = carry;
+                    carry = fma(e.p, carry, e.h);
+                }
+                return in;
+            }
+            Cols<V> pb = all_of<V>(1.0f), hb = all_of<V>(0.0f), pt = pb, ht = hb;                // of the groups ahead of this one; of all
+#pragma unroll
+            for (int i = 0; i < NG; ++i) {
+                const int j = DOWN ? NG - 1 - i : i;
+                const Maps<V> e = agg[buf][j][lane];
+                if (j == q) { pb = pt; hb = ht; }
+                if (i == 0) { pt = e.p; ht = e.h; }
+                else { ht = fma(e.p, ht, e.h); pt = mul(e.p, pt); }
+            }
+            for (int peer = q; peer < K; peer += NG) {
+                const unsigned to = cluster_address(&tot[buf][rank][lane], peer), bar = cluster_address(&bars[buf], peer);
+                if constexpr (V == 1) cluster_send(to, bar, pt.v[0], ht.v[0]); else cluster_send(to, bar, pt.v[0], pt.v[1], ht.v[0], ht.v[1]);
+            }
+            if (threadIdx.x == 0) barrier_expect(&bars[buf], K * LANES * (unsigned)sizeof(Maps<V>));
+            lost = lost || !barrier_wait(&bars[buf], (k >> 1) & 1);
+            const int ahead = DOWN ? K - 1 - rank : rank;
+#pragma unroll 4
+            for (int i = 0; i < ahead; ++i) {
+                const Maps<V> e = tot[buf][DOWN ? K - 1 - i : i][lane];
+                carry = fma(e.p, carry, e.h);
+            }
+            in = fma(pb, carry, hb);
+#pragma unroll 4
+            for (int i = ahead; i < K; ++i) {
+                const Maps<V> e = tot[buf][DOWN ? K - 1 - i : i][lane];
+                carry = fma(e.p, carry, e.h);
+            }
+            if (lost) in = carry = all_of<V>(__uint_as_float(0x7fffffffu));
+            return in;
+        }
+    }
 };
 
 // ---- forward -----------------------------------------------------------------------------------------------------------------
-template <class T, int V, int LX, int WR, int WC, int R, bool SAVE8>
-__global__ void __launch_bounds__(32 * WR * WC) scan_forward_kernel(const __grid_constant__ ScanArgs A) {
-    static_assert(!SAVE8 || (LX == 32 && R == 16), "a row's 32 columns of a scale lie in one warp; 16 scale bytes are one store");
+template <class T, int V, int LX, int WR, int WC, int R, bool SAVE8, bool MIX, class Off>
+__global__ void __launch_bounds__(32 * WR * WC, SAVE8 ? 3 : 4) scan_forward_kernel(const __grid_constant__ ScanArgs A) {
+    static_assert(!SAVE8 || (LX == 32 && R == 16), "a row's 32 columns of a scale lie in one warp, 16 rows' scales in 16 lanes");
     using Pl = Place<V, LX, WR, WC, R>;
     using W = Raw<T, V>;
-    constexpr int NG = Pl::NG, COLS = Pl::COLS, TILE = Pl::TILE;
-    __shared__ float aggP[2][NG > 1 ? NG : 1][NG > 1 ? COLS : 1], aggH[2][NG > 1 ? NG : 1][NG > 1 ? COLS : 1];
-    __shared__ float totP[2][SCAN_MOST_BLOCKS][NG > 1 ? COLS : 1], totH[2][SCAN_MOST_BLOCKS][NG > 1 ? COLS : 1];
+    constexpr int NG = Pl::NG, TILE = Pl::TILE, S = sizeof(T);
+    __shared__ Exchange<V, LX, WR, WC, R> ex;
     Pl at(A);
-    const int q = at.q, col = at.col, c = at.c, rank = at.rank;
+    const int q = at.q, c = at.c;
     const bool cv = at.cv;
     const int K = NG > 1 ? A.blocks : 1;
+    ex.init(K);
+    bool lost = false;
+    const float none = S == 4 ? 0.0f : least_decay();
     dep_wait();
     at.read_length(A);
     const int len = at.len;
     const int span = K * TILE;
     const int steps = (int)(((int64_t)len + span - 1) / span);
 
-    float carry[V];
+    Cols<V> carry;
 #pragma unroll
-    for (int v = 0; v < V; ++v) carry[v] = (A.start && cv) ? A.start[(int64_t)at.b * A.cols + c + v] : 0.0f;
+    for (int v = 0; v < V; ++v) carry.v[v] = (A.start && cv) ? A.start[(int64_t)at.b * A.cols + c + v] : 0.0f;
 
-    int t0 = rank * TILE + q * R;
-    const char* pg = A.g.p + at.b * A.g.batch + t0 * A.g.row + c * (int64_t)sizeof(T);
-    const char* px = A.x.p + at.b * A.x.batch + t0 * A.x.row + c * (int64_t)sizeof(T);
-    char* ph = A.h.p + at.b * A.h.batch + t0 * A.h.row + c * (int64_t)sizeof(T);
+    const char *const bg = at.base(A.g, S), *const bx = at.base(A.x, S);
+    char* const bh = at.base(A.h, S);
+    const Off og = at.template offset<Off>(A.g, S), ox = at.template offset<Off>(A.x, S), oh = at.template offset<Off>(A.h, S);
+    int row0 = at.rank * TILE;                             // of the block's tile; this thread's rows start at row0 + q R
 
     W rg[R], rx[R];
-    auto fetch = [&](int first) {
-        const int n = cv ? len - first : 0;
+    auto fetch = [&](int r0) {
+        const char *g = bg + r0 * A.g.row, *x = bx + r0 * A.x.row;
+        if (at.all && r0 + TILE <= len) {
 #pragma unroll
-        for (int i = 0; i < R; ++i) {
-            rg[i] = i < n ? load_at<W>(pg + i * A.g.row) : W(0);
-            rx[i] = i < n ? load_at<W>(px + i * A.x.row) : W(0);
+            for (int i = 0; i < R; ++i) {
+                rg[i] = load_at<W>(g + i * A.g.row + og);
+                rx[i] = load_at<W>(x + i * A.x.row + ox);
+            }
+        } else {
+            const int n = cv ? len - r0 - q * R : 0;
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                rg[i] = i < n ? load_at<W>(g + i * A.g.row + og) : W(0);
+                rx[i] = i < n ? load_at<W>(x + i * A.x.row + ox) : W(0);
+            }
         }
     };
-    if (steps > 0) fetch(t0);
-    if (K > 1) cluster_barrier();                          // every block of the cluster runs before one writes to another
+    if (steps > 0) fetch(row0);
+    if (K > 1) { cluster_arrive(); cluster_wait(); }       // every block of the cluster runs before one writes to another
 
-    for (int s = 0; s < steps; ++s) {
-        const int n = cv ? len - t0 : 0;                   // rows i < n hold data; the others pass the state on
-        float a[R][V], bb[R][V], P[V], H[V];
+    // Codes and scales of this warp's 16 rows.  The largest magnitudes of the 16 rows are found together: at every stage of a butterfly a lane
+    // hands half of its rows to the other and keeps the other's share of the rest, 15 exchanges of gate and input at once in place of 64
+    // or 80; lane r then holds row r, works out its scales, and hands them round.
+    [[maybe_unused]] auto encode = [&](auto full, int n) {
+        constexpr bool FULL = decltype(full)::value;
+        const int lane = threadIdx.x & 31, t0 = row0 + q * R;
+        uint32_t m[R];
 #pragma unroll
-        for (int v = 0; v < V; ++v) { P[v] = 1.0f; H[v] = 0.0f; }
-        uint32_t sg[SAVE8 ? 4 : 1] = {}, sx[SAVE8 ? 4 : 1] = {};
+        for (int i = 0; i < R; ++i) m[i] = magnitudes<T, V>(rg[i], rx[i]);
+#pragma unroll
+        for (int h = 8; h >= 1; h /= 2)
+#pragma unroll
+            for (int j = 0; j < h; ++j) {
+                const bool up = (lane & h) != 0;
+                const uint32_t keep = up ? m[j + h] : m[j], send = up ? m[j] : m[j + h];
+                m[j] = __vmaxu2(keep, __shfl_xor_sync(~0u, send, h));
+            }
+        if (V == 1) m[0] = __vmaxu2(m[0], __shfl_xor_sync(~0u, m[0], 16));
+        const int eg = exponent_of<T>(m[0] & 0xffffu), exx = exponent_of<T>(m[0] >> 16);
+        const int block = at.first / kBlock8 + (threadIdx.x >> 5) / WR * V + (V == 2 ? lane >> 4 : 0);
+        uint8_t *const gs = A.gs + ((int64_t)at.b * A.nblk + block) * A.rows_padded + t0, *const xs = A.xs + ((int64_t)at.b * A.nblk + block) * A.rows_padded + t0;
+        const bool mine = block < A.nblk && t0 < A.rows_padded;
+        uint8_t *const gq = A.gq + (((int64_t)at.b * A.rows + row0) * A.cols + at.first), *const xq = A.xq + (((int64_t)at.b * A.rows + row0) * A.cols + at.first);
+        const Off oq = (Off)(q * R) * (Off)A.cols + (Off)at.col;
+        if (__any_sync(~0u, eg == 255 || exx == 255)) {    // values that are not finite: row by row
+            const char *g = bg + row0 * A.g.row, *x = bx + row0 * A.x.row;
+#pragma unroll 1
+            for (int i = 0; i < R; ++i) {
+                const Cols<V> vg = expand<T, V>(i < n ? load_at<W>(g + i * A.g.row + og) : W(0)), vx = expand<T, V>(i < n ? load_at<W>(x + i * A.x.row + ox) : W(0));
+                unsigned mg = 0, mx = 0;
+#pragma unroll
+                for (int v = 0; v < V; ++v) { mg = max(mg, magnitude_bits(vg.v[v])); mx = max(mx, magnitude_bits(vx.v[v])); }
+#pragma unroll
+                for (int h = V == 2 ? 8 : 16; h >= 1; h /= 2) { mg = max(mg, __shfl_xor_sync(~0u, mg, h)); mx = max(mx, __shfl_xor_sync(~0u, mx, h)); }
+                const int sg = scale_byte(mg, true), sx = scale_byte(mx, A.int8);
+#pragma unroll
+                for (int v = 0; v < V; ++v)
+                    if (i < n) {
+                        gq[(int64_t)i * A.cols + oq + v] = (uint8_t)code_int8(vg.v[v], inverse_scale_of(sg));
+                        xq[(int64_t)i * A.cols + oq + v] = (uint8_t)code8(vx.v[v], inverse_scale_of(sx), A.int8);
+                    }
+                if (mine && (lane & (V == 2 ? 15 : 31)) == 0) { gs[i] = (uint8_t)sg; xs[i] = (uint8_t)sx; }
+            }
+            return;
+        }
+        const int sg = max(eg - 6, 1), sx = max(exx - (A.int8 ? 6 : 7), 1);
+        if (mine && (V == 2 || lane < 16)) { gs[lane & 15] = (uint8_t)sg; xs[lane & 15] = (uint8_t)sx; }
+        const uint32_t inverse = (uint32_t)(254 - sg) << 7 | (uint32_t)(254 - sx) << 23;            // upper halves of the two floats
 #pragma unroll
         for (int i = 0; i < R; ++i) {
-            float g[V], x[V];
-            expand<T, V>(rg[i], g);
-            expand<T, V>(rx[i], x);
-            if constexpr (SAVE8) {
-                unsigned mg = magnitude_bits(g[0]), mx = magnitude_bits(x[0]);
-                if constexpr (V == 2) {                    // two blocks of 32 columns in a warp's row
-                    mg = max(mg, magnitude_bits(g[1]));
-                    mx = max(mx, magnitude_bits(x[1]));
-                    const bool low = (threadIdx.x & 16) == 0;
-                    const unsigned g0 = __reduce_max_sync(~0u, low ? mg : 0u), g1 = __reduce_max_sync(~0u, low ? 0u : mg);
-                    const unsigned x0 = __reduce_max_sync(~0u, low ? mx : 0u), x1 = __reduce_max_sync(~0u, low ? 0u : mx);
-                    mg = low ? g0 : g1;
-                    mx = low ? x0 : x1;
-                } else {
-                    mg = __reduce_max_sync(~0u, mg);
-                    mx = __reduce_max_sync(~0u, mx);
-                }
-                const int bg = scale_byte(mg, true), bx = scale_byte(mx, A.int8);
-                sg[i / 4] |= (uint32_t)bg << (8 * (i % 4));
-                sx[i / 4] |= (uint32_t)bx << (8 * (i % 4));
-                if (i < n) {
-                    const float ig = inverse_scale_of(bg), ix = inverse_scale_of(bx);
-                    const int64_t o = ((int64_t)at.b * A.rows + t0 + i) * A.cols + c;
-                    if constexpr (V == 2) {
-                        *reinterpret_cast<uint16_t*>(A.gq + o) = (uint16_t)(code_int8(g[0], ig) | code_int8(g[1], ig) << 8);
-                        *reinterpret_cast<uint16_t*>(A.xq + o) = (uint16_t)(code8(x[0], ix, A.int8) | code8(x[1], ix, A.int8) << 8);
-                    } else {
-                        A.gq[o] = (uint8_t)code_int8(g[0], ig);
-                        A.xq[o] = (uint8_t)code8(x[0], ix, A.int8);
-                    }
-                }
-            }
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                float w;
-                gates<sizeof(T) == 4>(g[v], a[i][v], w);
-                bb[i][v] = A.mix ? w * x[v] : x[v];
-                if (i >= n) { a[i][v] = 1.0f; bb[i][v] = 0.0f; }
-                P[v] *= a[i][v];
-                H[v] = fmaf(a[i][v], H[v], bb[i][v]);
+            const uint32_t both = __shfl_sync(~0u, inverse, V == 2 ? (lane & 16) | i : i);
+            const uint32_t kg = codes_int8(expand<T, V>(rg[i]), __uint_as_float(both << 16));
+            const Cols<V> vx = expand<T, V>(rx[i]);
+            const float ix = __uint_as_float(both & 0xffff0000u);
+            const uint32_t kx = A.int8 ? codes_int8(vx, ix) : codes_e4m3(vx, ix);
+            if (FULL || i < n) {
+                using Q = std::conditional_t<V == 2, uint16_t, uint8_t>;
+                *reinterpret_cast<Q*>(gq + (int64_t)i * A.cols + oq) = (Q)kg;
+                *reinterpret_cast<Q*>(xq + (int64_t)i * A.cols + oq) = (Q)kx;
             }
         }
-        if constexpr (SAVE8) {
-            if ((threadIdx.x & (V == 2 ? 15 : 31)) == 0 && cv && t0 < A.rows_padded) {
-                const int64_t o = ((int64_t)at.b * A.nblk + c / kBlock8) * A.rows_padded + t0;
-                *reinterpret_cast<uint4*>(A.gs + o) = make_uint4(sg[0], sg[1], sg[2], sg[3]);
-                *reinterpret_cast<uint4*>(A.xs + o) = make_uint4(sx[0], sx[1], sx[2], sx[3]);
-            }
-        }
-        pg += span * A.g.row;
-        px += span * A.x.row;
-        if (s + 1 < steps) fetch(t0 + span);               // in flight while the states of this step are found
+    };
 
-        float hin[V];
-        if constexpr (NG == 1) {
+    Cols<V> a[R], bb[R], P, H;
+    // rows i < n of this thread hold data; the others (none in a full tile) pass the state on
+    auto prepare = [&](auto full, int n) {
+        constexpr bool FULL = decltype(full)::value;
+        if constexpr (SAVE8) encode(full, n);
 #pragma unroll
-            for (int v = 0; v < V; ++v) { hin[v] = carry[v]; carry[v] = fmaf(P[v], carry[v], H[v]); }
-        } else {
-            const int buf = s & 1;
-#pragma unroll
-            for (int v = 0; v < V; ++v) { aggP[buf][q][col + v] = P[v]; aggH[buf][q][col + v] = H[v]; }
-            __syncthreads();
-            if (K == 1) {
-#pragma unroll
-                for (int j = 0; j < NG; ++j)
-#pragma unroll
-                    for (int v = 0; v < V; ++v) {
-                        if (j == q) hin[v] = carry[v];
-                        carry[v] = fmaf(aggP[buf][j][col + v], carry[v], aggH[buf][j][col + v]);
-                    }
-            } else {
-                float Pb[V], Hb[V], Pt[V], Ht[V];          // of the groups ahead of this one; of all
-#pragma unroll
-                for (int v = 0; v < V; ++v) { Pb[v] = Pt[v] = 1.0f; Hb[v] = Ht[v] = 0.0f; }
-#pragma unroll
-                for (int j = 0; j < NG; ++j)
-#pragma unroll
-                    for (int v = 0; v < V; ++v) {
-                        if (j == q) { Pb[v] = Pt[v]; Hb[v] = Ht[v]; }
-                        const float p = aggP[buf][j][col + v];
-                        Ht[v] = fmaf(p, Ht[v], aggH[buf][j][col + v]);
-                        Pt[v] *= p;
-                    }
-                for (int peer = q; peer < K; peer += NG)
-#pragma unroll
-                    for (int v = 0; v < V; ++v) {
-                        cluster_store(cluster_address(&totP[buf][rank][col + v], peer), Pt[v]);
-                        cluster_store(cluster_address(&totH[buf][rank][col + v], peer), Ht[v]);
-                    }
-                cluster_barrier();
-                float hc[V] = {};
-                for (int peer = 0; peer < K; ++peer)
-#pragma unroll
-                    for (int v = 0; v < V; ++v) {
-                        if (peer == rank) hc[v] = carry[v];
-                        carry[v] = fmaf(totP[buf][peer][col + v], carry[v], totH[buf][peer][col + v]);
-                    }
-#pragma unroll
-                for (int v = 0; v < V; ++v) hin[v] = fmaf(Pb[v], hc[v], Hb[v]);
-            }
+        for (int i = 0; i < R; ++i) {
+            Cols<V> w;
+            gate_parts<T, V>(rg[i], a[i], w, none);
+            bb[i] = expand<T, V>(rx[i]);
+            if (MIX) bb[i] = mul(w, bb[i]);
+            if (!FULL && i >= n) { a[i] = all_of<V>(1.0f); bb[i] = all_of<V>(0.0f); }
+            P = i ? mul(P, a[i]) : a[i];
+            H = i ? fma(a[i], H, bb[i]) : bb[i];
         }
+    };
+
+    for (int s = 0; s < steps; ++s) {
+        const bool full = at.all && row0 + TILE <= len;
+        const int t0 = row0 + q * R, n = cv ? len - t0 : 0;
+        if (full) prepare(Yes{}, n); else prepare(No{}, n);
+        if (s + 1 < steps) fetch(row0 + span);             // in flight while the states of this step are found
+
+        Cols<V> hin = ex.template enter<false>(s, K, at.rank, q, at.col / V, P, H, carry, lost, [] {});
         if (A.states && cv && t0 % kChunkRows == 0 && t0 < A.rows) {
             float* st = A.states + ((int64_t)at.b * A.nchunk + t0 / kChunkRows) * A.cols + c;
 #pragma unroll
-            for (int v = 0; v < V; ++v) st[v] = hin[v];
+            for (int v = 0; v < V; ++v) st[v] = hin.v[v];
         }
-        const int m = cv ? A.rows - t0 : 0;
+        char* ph = bh + row0 * A.h.row;
+        if (full) {
 #pragma unroll
-        for (int i = 0; i < R; ++i) {
-            float out[V];
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                hin[v] = fmaf(a[i][v], hin[v], bb[i][v]);
-                out[v] = i < n ? hin[v] : 0.0f;
+            for (int i = 0; i < R; ++i) {
+                hin = fma(a[i], hin, bb[i]);
+                store_at<W>(ph + i * A.h.row + oh, join<T, V>(hin));
             }
-            if (i < m) store_at<W>(ph + i * A.h.row, join<T, V>(out));
-        }
-        ph += span * A.h.row;
-        t0 += span;
-    }
-    for (; t0 < A.rows; t0 += span, ph += span * A.h.row)  // rows behind a sequence
-        for (int i = 0; i < R && i < A.rows - t0; ++i)
-            if (cv) store_at<W>(ph + i * A.h.row, W(0));
-    if (A.end && rank == 0 && q == 0 && cv) {
+        } else {
+            const int m = cv ? A.rows - t0 : 0;
 #pragma unroll
-        for (int v = 0; v < V; ++v) A.end[(int64_t)at.b * A.cols + c + v] = carry[v];
+            for (int i = 0; i < R; ++i) {
+                hin = fma(a[i], hin, bb[i]);
+                if (i < m) store_at<W>(ph + i * A.h.row + oh, i < n ? join<T, V>(hin) : W(0));
+            }
+        }
+        row0 += span;
     }
+    for (; row0 < A.rows; row0 += span)                    // rows behind a sequence
+        for (int i = 0; i < R && i < A.rows - row0 - q * R; ++i)
+            if (cv) store_at<W>(bh + (row0 + i) * A.h.row + oh, W(0));
+    if (A.end && at.rank == 0 && q == 0 && cv) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) A.end[(int64_t)at.b * A.cols + c + v] = carry.v[v];
+    }
+    if (K > 1) { cluster_arrive(); cluster_wait(); }       // no block's shared memory goes while another could write to it
 }
 
 // ---- backward ----------------------------------------------------------------------------------------------------------------
-template <class T, int V, int LX, int WR, int WC, bool SAVED8>
-__global__ void __launch_bounds__(32 * WR * WC) scan_backward_kernel(const __grid_constant__ ScanArgs A) {
+template <class T, int V, int LX, int WR, int WC, bool SAVED8, bool MIX, class Off>
+__global__ void __launch_bounds__(32 * WR * WC, 16 / (WR * WC)) scan_backward_kernel(const __grid_constant__ ScanArgs A) {
     constexpr int R = 8, GC = kChunkRows / R;              // 8 scale bytes are one load; groups of a chunk
     using Pl = Place<V, LX, WR, WC, R>;
     using W = Raw<T, V>;
     using Q = std::conditional_t<V == 2, uint16_t, uint8_t>;
-    constexpr int NG = Pl::NG, COLS = Pl::COLS, TILE = Pl::TILE;
+    constexpr int NG = Pl::NG, TILE = Pl::TILE, S = sizeof(T);
     static_assert(NG == 1 || TILE % kChunkRows == 0, "a tile holds whole chunks, or is the only one");
-    constexpr int SG = NG > 1 ? NG : 1, SC = NG > 1 ? COLS : 1;
-    __shared__ float aggP[2][SG][SC], aggH[2][SG][SC], aggM[2][SG][SC];
-    __shared__ float totP[2][SCAN_MOST_BLOCKS][SC], totM[2][SCAN_MOST_BLOCKS][SC];
+    __shared__ Exchange<V, LX, WR, WC, R> ex;
+    __shared__ Cols<V> aggH[2][NG > 1 ? NG : 1][NG > 1 ? WC * LX : 1];
     Pl at(A);
-    const int q = at.q, col = at.col, c = at.c, rank = at.rank;
+    const int q = at.q, c = at.c, lane = at.col / V;
     const bool cv = at.cv;
     const int K = NG > 1 ? A.blocks : 1;
+    ex.init(K);
+    bool lost = false;
+    const float none = S == 4 ? 0.0f : least_decay();
     dep_wait();
     at.read_length(A);
     const int len = at.len;
     const int span = K * TILE;
     const int steps = (int)(((int64_t)len + span - 1) / span);
 
-    float carry[V];                                        // mu of the row behind
+    Cols<V> carry;                                         // mu of the row behind
 #pragma unroll
-    for (int v = 0; v < V; ++v) carry[v] = (A.start && cv) ? A.start[(int64_t)at.b * A.cols + c + v] : 0.0f;
+    for (int v = 0; v < V; ++v) carry.v[v] = (A.start && cv) ? A.start[(int64_t)at.b * A.cols + c + v] : 0.0f;
 
-    for (int t = steps * span + rank * TILE + q * R; t < A.rows; t += span)          // rows behind a sequence
-        for (int i = 0; i < R && i < A.rows - t; ++i)
+    const char *const bg = SAVED8 ? nullptr : at.base(A.g, S), *const bx = SAVED8 ? nullptr : at.base(A.x, S), *const bd = A.dh.p ? at.base(A.dh, S) : nullptr;
+    char *const bdg = at.base(A.dg, S), *const bdx = at.base(A.dx, S);
+    const Off og = at.template offset<Off>(A.g, S), ox = at.template offset<Off>(A.x, S), od = at.template offset<Off>(A.dh, S);
+    const Off odg = at.template offset<Off>(A.dg, S), odx = at.template offset<Off>(A.dx, S), oq = (Off)(q * R) * (Off)A.cols + (Off)at.col;
+
+    for (int r0 = steps * span + at.rank * TILE; r0 < A.rows; r0 += span)            // rows behind a sequence
+        for (int i = 0; i < R && i < A.rows - r0 - q * R; ++i)
             if (cv) {
-                store_at<W>(A.dg.p + at.b * A.dg.batch + (t + i) * A.dg.row + c * (int64_t)sizeof(T), W(0));
-                store_at<W>(A.dx.p + at.b * A.dx.batch + (t + i) * A.dx.row + c * (int64_t)sizeof(T), W(0));
+                store_at<W>(bdg + (r0 + i) * A.dg.row + odg, W(0));
+                store_at<W>(bdx + (r0 + i) * A.dx.row + odx, W(0));
             }
 
-    int t0 = (steps - 1) * span + rank * TILE + q * R;
+    int row0 = (steps - 1) * span + at.rank * TILE;
     W rg[SAVED8 ? 1 : R], rx[SAVED8 ? 1 : R], rd[R];
     Q qg[SAVED8 ? R : 1], qx[SAVED8 ? R : 1];
     uint2 sg{}, sx{};
-    float st[V];
+    Cols<V> st;
     const int qc = NG > 1 ? q % GC : 0;                    // groups of the same chunk ahead of this one
-    auto fetch = [&](int first) {
-        const int n = cv ? len - first : 0;
+    auto fetch_rows = [&](auto full, int r0) {
+        constexpr bool FULL = decltype(full)::value;
+        const int t = r0 + q * R, n = cv ? len - t : 0;
         if constexpr (SAVED8) {
-            const int64_t o = ((int64_t)at.b * A.rows + first) * A.cols + c;
-            const int64_t os = ((int64_t)at.b * A.nblk + c / kBlock8) * A.rows_padded + first;
-            if (n > 0) { sg = *reinterpret_cast<const uint2*>(A.gs + os); sx = *reinterpret_cast<const uint2*>(A.xs + os); }
+            const int64_t o = ((int64_t)at.b * A.rows + r0) * A.cols + at.first;
+            if (FULL || n > 0) {
+                const int64_t os = ((int64_t)at.b * A.nblk + c / kBlock8) * A.rows_padded + t;
+                sg = *reinterpret_cast<const uint2*>(A.gs + os);
+                sx = *reinterpret_cast<const uint2*>(A.xs + os);
+            }
 #pragma unroll
             for (int i = 0; i < R; ++i) {
-                qg[i] = i < n ? *reinterpret_cast<const Q*>(A.gq + o + (int64_t)i * A.cols) : Q(0);
-                qx[i] = i < n ? *reinterpret_cast<const Q*>(A.xq + o + (int64_t)i * A.cols) : Q(0);
+                qg[i] = FULL || i < n ? *reinterpret_cast<const Q*>(A.gq + (o + (int64_t)i * A.cols) + oq) : Q(0x8080);
+                qx[i] = FULL || i < n ? *reinterpret_cast<const Q*>(A.xq + (o + (int64_t)i * A.cols) + oq) : Q(0x8080);
             }
         } else {
-            const char* pg = A.g.p + at.b * A.g.batch + first * A.g.row + c * (int64_t)sizeof(T);
-            const char* px = A.x.p + at.b * A.x.batch + first * A.x.row + c * (int64_t)sizeof(T);
+            const char *g = bg + r0 * A.g.row, *x = bx + r0 * A.x.row;
 #pragma unroll
             for (int i = 0; i < R; ++i) {
-                rg[i] = i < n ? load_at<W>(pg + i * A.g.row) : W(0);
-                rx[i] = i < n ? load_at<W>(px + i * A.x.row) : W(0);
+                rg[i] = FULL || i < n ? load_at<W>(g + i * A.g.row + og) : W(0);
+                rx[i] = FULL || i < n ? load_at<W>(x + i * A.x.row + ox) : W(0);
             }
         }
-        const char* pd = A.dh.p + at.b * A.dh.batch + first * A.dh.row + c * (int64_t)sizeof(T);
-        const int nd = A.dh.p ? n : 0;
+        const char* d = bd + r0 * A.dh.row;
 #pragma unroll
-        for (int i = 0; i < R; ++i) rd[i] = i < nd ? load_at<W>(pd + i * A.dh.row) : W(0);
-        const float* ps = A.states + ((int64_t)at.b * A.nchunk + first / kChunkRows) * A.cols + c;
+        for (int i = 0; i < R; ++i) rd[i] = (FULL || i < n) && bd ? load_at<W>(d + i * A.dh.row + od) : W(0);
+        const float* ps = A.states + ((int64_t)at.b * A.nchunk + t / kChunkRows) * A.cols + c;
 #pragma unroll
-        for (int v = 0; v < V; ++v) st[v] = n > 0 ? ps[v] : 0.0f;
+        for (int v = 0; v < V; ++v) st.v[v] = FULL || n > 0 ? ps[v] : 0.0f;
     };
-    if (steps > 0) fetch(t0);
-    if (K > 1) cluster_barrier();
+    auto fetch = [&](int r0) {
+        if (at.all && r0 + TILE <= len) fetch_rows(Yes{}, r0); else fetch_rows(No{}, r0);
+    };
+    if (steps > 0) fetch(row0);
+    if (K > 1) { cluster_arrive(); cluster_wait(); }
 
-    for (int s = steps - 1; s >= 0; --s) {
-        const int n = cv ? len - t0 : 0;
-        float a[R][V], w[R][V], x[R][V], d[R][V], P[V], H[V], M[V], hin[V];
+    Cols<V> a[R], w[R], x[R], d[R], P, H, M;
+    auto prepare = [&](auto full, int n) {
+        constexpr bool FULL = decltype(full)::value;
+        uint32_t zero_g = 0, zero_x = 0;
+        if constexpr (SAVED8) {
+            constexpr int PER = 4 / V;                     // rows whose codes fill a word
 #pragma unroll
-        for (int v = 0; v < V; ++v) { P[v] = 1.0f; H[v] = 0.0f; M[v] = 0.0f; hin[v] = st[v]; }
+            for (int i = 0; i < R; i += PER) {
+                uint32_t wg = 0, wx = 0;
+#pragma unroll
+                for (int j = 0; j < PER; ++j) { wg |= (uint32_t)qg[i + j] << (8 * V * j); wx |= (uint32_t)qx[i + j] << (8 * V * j); }
+                zero_g |= any_zero_byte(wg);
+                zero_x |= any_zero_byte(wx);
+            }
+            if (!A.int8) zero_x = 0;
+        }
 #pragma unroll
         for (int i = 0; i < R; ++i) {
-            float g[V];
             if constexpr (SAVED8) {
-                const float fg = scale_of(((i < 4 ? sg.x : sg.y) >> (8 * (i % 4))) & 255), fx = scale_of(((i < 4 ? sx.x : sx.y) >> (8 * (i % 4))) & 255);
+                const uint32_t bytes_g = i < 4 ? sg.x : sg.y, bytes_x = i < 4 ? sx.x : sx.y;
+                const float fg = scale_of((bytes_g >> (8 * (i % 4))) & 255), fx = scale_of((bytes_x >> (8 * (i % 4))) & 255);
+                Cols<V> g = values_int8<V>(qg[i], fg);
+                x[i] = A.int8 ? values_int8<V>(qx[i], fx) : values_e4m3<V>(qx[i], fx);
+                if (zero_g | zero_x) {                     // rare: some value of this thread was not finite
 #pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    g[v] = value_int8((qg[i] >> (8 * v)) & 255, fg);
-                    x[i][v] = value8((qx[i] >> (8 * v)) & 255, fx, A.int8);
+                    for (int v = 0; v < V; ++v) {
+                        if (((qg[i] >> (8 * v)) & 255) == 0) g.v[v] = __uint_as_float(0x7fffffffu);
+                        if (A.int8 && ((qx[i] >> (8 * v)) & 255) == 0) x[i].v[v] = __uint_as_float(0x7fffffffu);
+                    }
                 }
+                gates<S == 4>(g, a[i], w[i], none);
             } else {
-                expand<T, V>(rg[i], g);
-                expand<T, V>(rx[i], x[i]);
+                gate_parts<T, V>(rg[i], a[i], w[i], none);
+                x[i] = expand<T, V>(rx[i]);
             }
-            expand<T, V>(rd[i], d[i]);
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                gates<sizeof(T) == 4>(g[v], a[i][v], w[i][v]);
-                if (i >= n) { a[i][v] = 1.0f; w[i][v] = 0.0f; x[i][v] = 0.0f; }
-                P[v] *= a[i][v];
-                H[v] = fmaf(a[i][v], H[v], A.mix ? w[i][v] * x[i][v] : x[i][v]);
-            }
+            d[i] = expand<T, V>(rd[i]);
+            if (!FULL && i >= n) { a[i] = all_of<V>(1.0f); w[i] = x[i] = all_of<V>(0.0f); }
+            const Cols<V> in = MIX ? mul(w[i], x[i]) : x[i];
+            P = i ? mul(P, a[i]) : a[i];
+            H = i ? fma(a[i], H, in) : in;
         }
 #pragma unroll
-        for (int i = R - 1; i >= 0; --i)
-#pragma unroll
-            for (int v = 0; v < V; ++v) M[v] = a[i][v] * (d[i][v] + M[v]);
-        if (s > 0) fetch(t0 - span);
-
-        float mu[V];
-        if constexpr (NG == 1) {
-#pragma unroll
-            for (int v = 0; v < V; ++v) { mu[v] = carry[v]; carry[v] = fmaf(P[v], carry[v], M[v]); }
-        } else {
-            const int buf = s & 1;
-#pragma unroll
-            for (int v = 0; v < V; ++v) { aggP[buf][q][col + v] = P[v]; aggH[buf][q][col + v] = H[v]; aggM[buf][q][col + v] = M[v]; }
-            __syncthreads();
-            for (int j = q - qc; j < q; ++j)
-#pragma unroll
-                for (int v = 0; v < V; ++v) hin[v] = fmaf(aggP[buf][j][col + v], hin[v], aggH[buf][j][col + v]);
-            if (K == 1) {
-#pragma unroll
-                for (int j = NG - 1; j >= 0; --j)
-#pragma unroll
-                    for (int v = 0; v < V; ++v) {
-                        if (j == q) mu[v] = carry[v];
-                        carry[v] = fmaf(aggP[buf][j][col + v], carry[v], aggM[buf][j][col + v]);
-                    }
-            } else {
-                float Pb[V], Mb[V], Pt[V], Mt[V];
-#pragma unroll
-                for (int v = 0; v < V; ++v) { Pb[v] = Pt[v] = 1.0f; Mb[v] = Mt[v] = 0.0f; }
-#pragma unroll
-                for (int j = NG - 1; j >= 0; --j)
-#pragma unroll
-                    for (int v = 0; v < V; ++v) {
-                        if (j == q) { Pb[v] = Pt[v]; Mb[v] = Mt[v]; }
-                        const float p = aggP[buf][j][col + v];
-                        Mt[v] = fmaf(p, Mt[v], aggM[buf][j][col + v]);
-                        Pt[v] *= p;
-                    }
-                for (int peer = q; peer < K; peer += NG)
-#pragma unroll
-                    for (int v = 0; v < V; ++v) {
-                        cluster_store(cluster_address(&totP[buf][rank][col + v], peer), Pt[v]);
-                        cluster_store(cluster_address(&totM[buf][rank][col + v], peer), Mt[v]);
-                    }
-                cluster_barrier();
-                float mc[V] = {};
-                for (int peer = K - 1; peer >= 0; --peer)
-#pragma unroll
-                    for (int v = 0; v < V; ++v) {
-                        if (peer == rank) mc[v] = carry[v];
-                        carry[v] = fmaf(totP[buf][peer][col + v], carry[v], totM[buf][peer][col + v]);
-                    }
-#pragma unroll
-                for (int v = 0; v < V; ++v) mu[v] = fmaf(Pb[v], mc[v], Mb[v]);
-            }
-        }
-        // x <- a (1 - a) (h_{t-1} [- x]), the factor of dg
-#pragma unroll
-        for (int i = 0; i < R; ++i)
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const float in = A.mix ? w[i][v] * x[i][v] : x[i][v];
-                const float diff = A.mix ? hin[v] - x[i][v] : hin[v];
-                hin[v] = fmaf(a[i][v], hin[v], in);
-                x[i][v] = a[i][v] * w[i][v] * diff;
-            }
-        const int m = cv ? A.rows - t0 : 0;
-        char* pdg = A.dg.p + at.b * A.dg.batch + t0 * A.dg.row + c * (int64_t)sizeof(T);
-        char* pdx = A.dx.p + at.b * A.dx.batch + t0 * A.dx.row + c * (int64_t)sizeof(T);
+        for (int i = R - 1; i >= 0; --i) M = mul(a[i], i < R - 1 ? add(d[i], M) : d[i]);
+    };
+    auto write = [&](auto full, int n, int m, Cols<V> mu) {
+        constexpr bool FULL = decltype(full)::value;
+        char *pdg = bdg + row0 * A.dg.row, *pdx = bdx + row0 * A.dx.row;
 #pragma unroll
         for (int i = R - 1; i >= 0; --i) {
-            float og[V], ox[V];
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const float lam = d[i][v] + mu[v];
-                og[v] = i < n ? lam * x[i][v] : 0.0f;
-                ox[v] = i < n ? (A.mix ? lam * w[i][v] : lam) : 0.0f;
-                mu[v] = a[i][v] * lam;
-            }
-            if (i < m) {
-                store_at<W>(pdg + i * A.dg.row, join<T, V>(og));
-                store_at<W>(pdx + i * A.dx.row, join<T, V>(ox));
+            const Cols<V> lam = add(d[i], mu), og_ = mul(lam, x[i]), ox_ = MIX ? mul(lam, w[i]) : lam;
+            mu = mul(a[i], lam);
+            if (FULL || i < m) {
+                store_at<W>(pdg + i * A.dg.row + odg, FULL || i < n ? join<T, V>(og_) : W(0));
+                store_at<W>(pdx + i * A.dx.row + odx, FULL || i < n ? join<T, V>(ox_) : W(0));
             }
         }
-        t0 -= span;
-    }
-    if (A.end && rank == 0 && q == 0 && cv) {
+    };
+
+    for (int s = steps - 1; s >= 0; --s) {
+        const bool full = at.all && row0 + TILE <= len;
+        const int t0 = row0 + q * R, n = cv ? len - t0 : 0, k = steps - 1 - s, buf = k & 1;
+        Cols<V> hin = st;
+        if (full) prepare(Yes{}, n); else prepare(No{}, n);
+        if (s > 0) fetch(row0 - span);
+
+        if constexpr (NG > 1) aggH[buf][q][lane] = H;
+        const Cols<V> mu = ex.template enter<true>(k, K, at.rank, q, lane, P, M, carry, lost, [&] {
+            if constexpr (NG > 1)
+                for (int j = q - qc; j < q; ++j) hin = fma(ex.agg[buf][j][lane].p, hin, aggH[buf][j][lane]);
+        });
+        // x <- a (1 - a) (h_{t-1} [- x]), the factor of dg
 #pragma unroll
-        for (int v = 0; v < V; ++v) A.end[(int64_t)at.b * A.cols + c + v] = carry[v];
+        for (int i = 0; i < R; ++i) {
+            const Cols<V> in = MIX ? mul(w[i], x[i]) : x[i];
+            const Cols<V> diff = MIX ? fma(x[i], all_of<V>(-1.0f), hin) : hin;
+            hin = fma(a[i], hin, in);
+            x[i] = mul(mul(a[i], w[i]), diff);
+        }
+        const int m = cv ? A.rows - t0 : 0;
+        if (full) write(Yes{}, n, m, mu); else write(No{}, n, m, mu);
+        row0 -= span;
     }
+    if (A.end && at.rank == 0 && q == 0 && cv) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) A.end[(int64_t)at.b * A.cols + c + v] = carry.v[v];
+    }
+    if (K > 1) { cluster_arrive(); cluster_wait(); }
 }
 
 // ---- launches ----------------------------------------------------------------------------------------------------------------
@@ -469,40 +572,99 @@ template <int V, int LX, int WR, int WC, int R> Shape shape_of(Kernel k, bool sp
     return Shape{k, Pl::COLS, Pl::TILE, Pl::THREADS, split};
 }
 
-enum Layout { ONE_ROW, SHORT, TALL, NARROW };
+enum Layout { ONE_ROW, SHORT, TALL, NARROW, TALL_FAR };    // TALL_FAR: rows so far apart that offsets within a tile take 64 bits
 
-template <class T, int V> Shape forward_shape(Layout l, bool save8) {
-    if (save8) return l == SHORT ? shape_of<V, 32, 1, 4, 16>(scan_forward_kernel<T, V, 32, 1, 4, 16, true>, false)
-                                 : shape_of<V, 32, 4, 1, 16>(scan_forward_kernel<T, V, 32, 4, 1, 16, true>, true);
+template <class T, int V, bool MIX> Shape forward_shape(Layout l, bool save8) {
+    using Near = uint32_t;
+    using Far = int64_t;
+    if (save8) switch (l) {
+        case ONE_ROW:
+        case SHORT: return shape_of<V, 32, 1, 4, 16>(scan_forward_kernel<T, V, 32, 1, 4, 16, true, MIX, Near>, false);
+        case TALL_FAR: return shape_of<V, 32, 4, 1, 16>(scan_forward_kernel<T, V, 32, 4, 1, 16, true, MIX, Far>, true);
+        default: return shape_of<V, 32, 4, 1, 16>(scan_forward_kernel<T, V, 32, 4, 1, 16, true, MIX, Near>, true);
+    }
     switch (l) {
-        case ONE_ROW: return shape_of<V, 32, 1, 4, 1>(scan_forward_kernel<T, V, 32, 1, 4, 1, false>, false);
-        case SHORT: return shape_of<V, 32, 1, 4, 16>(scan_forward_kernel<T, V, 32, 1, 4, 16, false>, false);
-        case TALL: return shape_of<V, 32, 4, 1, 16>(scan_forward_kernel<T, V, 32, 4, 1, 16, false>, true);
-        default: return shape_of<V, 8, 4, 1, 16>(scan_forward_kernel<T, V, 8, 4, 1, 16, false>, true);
+        case ONE_ROW: return shape_of<V, 32, 1, 4, 1>(scan_forward_kernel<T, V, 32, 1, 4, 1, false, MIX, Near>, false);
+        case SHORT: return shape_of<V, 32, 1, 4, 16>(scan_forward_kernel<T, V, 32, 1, 4, 16, false, MIX, Near>, false);
+        case TALL: return shape_of<V, 32, 4, 1, 16>(scan_forward_kernel<T, V, 32, 4, 1, 16, false, MIX, Near>, true);
+        case TALL_FAR: return shape_of<V, 32, 4, 1, 16>(scan_forward_kernel<T, V, 32, 4, 1, 16, false, MIX, Far>, true);
+        default: return shape_of<V, 8, 4, 1, 16>(scan_forward_kernel<T, V, 8, 4, 1, 16, false, MIX, Near>, true);
     }
 }
-template <class T, int V, bool SAVED8> Shape backward_shape(Layout l) {
+template <class T, int V, bool SAVED8, bool MIX> Shape backward_shape(Layout l) {
+    using Near = uint32_t;
+    using Far = int64_t;
     switch (l) {
         case ONE_ROW:
-        case SHORT: return shape_of<V, 32, 1, 4, 8>(scan_backward_kernel<T, V, 32, 1, 4, SAVED8>, false);
-        case TALL: return shape_of<V, 32, 8, 1, 8>(scan_backward_kernel<T, V, 32, 8, 1, SAVED8>, true);
-        default: return shape_of<V, 8, 8, 1, 8>(scan_backward_kernel<T, V, 8, 8, 1, SAVED8>, true);
+        case SHORT: return shape_of<V, 32, 1, 4, 8>(scan_backward_kernel<T, V, 32, 1, 4, SAVED8, MIX, Near>, false);
+        case TALL: return shape_of<V, 32, 8, 1, 8>(scan_backward_kernel<T, V, 32, 8, 1, SAVED8, MIX, Near>, true);
+        case TALL_FAR: return shape_of<V, 32, 8, 1, 8>(scan_backward_kernel<T, V, 32, 8, 1, SAVED8, MIX, Far>, true);
+        default: return shape_of<V, 8, 8, 1, 8>(scan_backward_kernel<T, V, 8, 8, 1, SAVED8, MIX, Near>, true);
     }
+}
+template <class T, int V> Shape shape_for(bool mix, bool forward, bool save8, Layout l) {
+    if (forward) return mix ? forward_shape<T, V, true>(l, save8) : forward_shape<T, V, false>(l, save8);
+    if (save8) return mix ? backward_shape<T, V, true, true>(l) : backward_shape<T, V, true, false>(l);
+    return mix ? backward_shape<T, V, false, true>(l) : backward_shape<T, V, false, false>(l);
 }
 
 Shape pick(const dn_scan& s, bool pairs, bool forward, bool save8, Layout l) {
+    const bool mix = (s.flags & DN_SCAN_MIX) != 0;
     switch (s.type) {
-        case DN_F32: return forward ? forward_shape<float, 1>(l, save8) : save8 ? backward_shape<float, 1, true>(l) : backward_shape<float, 1, false>(l);
-        case DN_BF16:
-            if (pairs) return forward ? forward_shape<__nv_bfloat16, 2>(l, save8) : save8 ? backward_shape<__nv_bfloat16, 2, true>(l) : backward_shape<__nv_bfloat16, 2, false>(l);
-            return forward ? forward_shape<__nv_bfloat16, 1>(l, save8) : save8 ? backward_shape<__nv_bfloat16, 1, true>(l) : backward_shape<__nv_bfloat16, 1, false>(l);
-        default:
-            if (pairs) return forward ? forward_shape<__half, 2>(l, save8) : save8 ? backward_shape<__half, 2, true>(l) : backward_shape<__half, 2, false>(l);
-            return forward ? forward_shape<__half, 1>(l, save8) : save8 ? backward_shape<__half, 1, true>(l) : backward_shape<__half, 1, false>(l);
+        case DN_F32: return shape_for<float, 1>(mix, forward, save8, l);
+        case DN_BF16: return pairs ? shape_for<__nv_bfloat16, 2>(mix, forward, save8, l) : shape_for<__nv_bfloat16, 1>(mix, forward, save8, l);
+        default: return pairs ? shape_for<__half, 2>(mix, forward, save8, l) : shape_for<__half, 1>(mix, forward, save8, l);
     }
 }
 
 constexpr int64_t MOST_GRID = 0x7fffffff;
+
+// Clusters of `blocks` blocks that the device holds at a time.
+int active_clusters(const Shape& f, int blocks) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(blocks); cfg.blockDim = dim3(f.threads);
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = (unsigned)blocks; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
+    cfg.attrs = at; cfg.numAttrs = 1;
+    int n = 0;
+    if (cudaFuncSetAttribute(f.kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess ||
+        cudaOccupancyMaxActiveClusters(&n, f.kernel, &cfg) != cudaSuccess) { (void)cudaGetLastError(); return 0; }
+    return n;
+}
+
+// Blocks per cluster for n strips of columns, by an estimate of the time.  A step takes one latency (of loads, arithmetic and exchange),
+// and with all slots of an SM taken about two: measured, 1.2 to 1.4 us for one block per SM, 1.9 for two and 2.1 for 3.4 of 4 (64 rows
+// of 64 columns in 16 bits).  Two steps' time is added per wave for its start, 3 % per block that the others wait for.  32 strips of
+// 65536 rows: 1260 us with a block each, 364 with 4, 243 with 8; 16 take 272, since only 31 such clusters fit the device at a time.
+int blocks_for(const Shape& f, int64_t n, int rows) {
+    struct Known { Kernel kernel; int dev, rows, blocks; int64_t n; };
+    constexpr int KEPT = 16;
+    thread_local Known known[KEPT] = {};                   // the last few answers: a function of the arguments and the device
+    thread_local int next = 0;
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) { (void)cudaGetLastError(); return 1; }
+    for (const Known& k : known)
+        if (k.kernel == f.kernel && k.dev == dev && k.rows == rows && k.n == n) return k.blocks;
+    const double sms = sm_count();
+    const int64_t most = ((int64_t)rows + f.tile - 1) / f.tile;
+    int best = 1;
+    double least = 0.0, slots = 0.0;
+    for (int k = 1; k <= SCAN_MOST_BLOCKS && k <= most; ++k) {
+        const int64_t active = active_clusters(f, k);
+        if (active < 1) continue;
+        if (k == 1) slots = active / sms;
+        const double waves = n < 3 * active ? (double)((n + active - 1) / active) : (double)n / active;
+        const double steps = (double)((rows + (int64_t)k * f.tile - 1) / ((int64_t)k * f.tile));
+        const double taken = (double)(n < active ? n : active) * k / sms;
+        const double t = waves * (steps + 2.0) * (1.0 + taken / slots) * (1.0 + 0.03 * (k - 1));
+        if (k == 1 || t < least) { least = t; best = k; }
+        if (waves > 4.0) break;                            // strips enough to fill the device several times
+    }
+    known[next] = Known{f.kernel, dev, rows, best, n};
+    next = (next + 1) % KEPT;
+    return best;
+}
 
 // Layout and blocks per cluster.  A sample's strip of columns is marched by one block where there are enough strips to fill the
 // device, else by a cluster along the rows; where even clusters of 16 leave SMs idle, strips of 8 lanes.
@@ -512,15 +674,19 @@ dn_status launch(const dn_scan& s, bool pairs, bool forward, ScanArgs& A, cudaSt
     auto units = [&](const Shape& f) { return (((int64_t)s.cols + f.cols - 1) / f.cols) * s.batch; };
     Layout l = s.rows <= (forward ? 16 : 8) ? (s.rows <= 1 && !save8 ? ONE_ROW : SHORT) : TALL;
     Shape f = pick(s, pairs, forward, save8, l);
-    if (l == TALL && !(forward && save8) && units(f) * SCAN_MOST_BLOCKS < sms) f = pick(s, pairs, forward, save8, NARROW);
+    if (l == TALL) {
+        int64_t row = save8 ? s.cols : 0;                  // bytes between rows, at most
+        for (const RowsOf& r : {A.g, A.x, A.h, A.dh, A.dg, A.dx}) row = r.row > row ? r.row : row;
+        const bool far = (row + 1) * 64 + 4096 > (int64_t)UINT32_MAX, very = (row + 1) * 256 + 4096 > (int64_t)UINT32_MAX;
+        if (far) f = pick(s, pairs, forward, save8, TALL_FAR);
+        else if (!very && !(forward && save8) && units(f) * SCAN_MOST_BLOCKS < sms) f = pick(s, pairs, forward, save8, NARROW);
+    }
     int blocks = 1;
     const int64_t n = units(f);
-    if (f.split)
-        while (blocks < SCAN_MOST_BLOCKS && n * blocks < 4 * sms && (int64_t)blocks * f.tile < s.rows) blocks *= 2;
+    if (f.split) blocks = blocks_for(f, n, s.rows);
     if (n * blocks > MOST_GRID) return DN_ERR_SIZE;
     A.strips = (s.cols + f.cols - 1) / f.cols;
     A.blocks = blocks;
-    if (blocks > 8 && cudaFuncSetAttribute(f.kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) { (void)cudaGetLastError(); return DN_ERR_CUDA; }
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(n * blocks)); cfg.blockDim = dim3(f.threads); cfg.stream = stream;
     cudaLaunchAttribute attr[2];
@@ -641,7 +807,7 @@ dn_status dn_scan_forward(const dn_scan* s, const dn_rows* g, const dn_rows* x, 
     A.g = rows_of(*s, g); A.x = rows_of(*s, x); A.h = rows_of(*s, h);
     A.start = h0; A.end = h_last; A.lengths = s->lengths;
     A.rows = s->rows; A.cols = s->cols;
-    A.mix = (s->flags & DN_SCAN_MIX) != 0; A.int8 = q.format == DN_INT8;
+    A.int8 = q.format == DN_INT8;
     const bool pairs = s->type != DN_F32 && s->cols % 2 == 0 && paired(*s, g) && paired(*s, x) && paired(*s, h);
     return launch(q, pairs, true, A, static_cast<cudaStream_t>(stream));
 }
@@ -674,7 +840,7 @@ dn_status dn_scan_backward(const dn_scan* s, const dn_rows* g, const dn_rows* x,
     A.g = rows_of(*s, &in_g); A.x = rows_of(*s, &in_x); A.dh = rows_of(*s, &in_d); A.dg = rows_of(*s, dg); A.dx = rows_of(*s, dx);
     A.start = dh_last; A.end = dh0; A.lengths = s->lengths;
     A.rows = s->rows; A.cols = s->cols;
-    A.mix = (s->flags & DN_SCAN_MIX) != 0; A.int8 = s->format == DN_INT8;
+    A.int8 = s->format == DN_INT8;
     const bool pairs = s->type != DN_F32 && s->cols % 2 == 0 && paired(*s, &in_g) && paired(*s, &in_x) && paired(*s, &in_d) && paired(*s, dg) && paired(*s, dx);
     return launch(*s, pairs, false, A, static_cast<cudaStream_t>(stream));
 }
