@@ -26,19 +26,17 @@ class Packed:
 
     def unpack(self) -> torch.Tensor:
         """The values that stand for the tensor: contiguous, of its type, on its device."""
-        out = torch.empty(self.shape, dtype=self.dtype, device=self.data.device)
-        if out.numel():
-            B.dn_unpack(self.data, self.format, out)
+        out = B.native().unpacked(self.data, B._format(self.format), self.shape, self.dtype)
+        if isinstance(out, int):
+            raise B.DnError(out, "dn_unpack")
         return out
 
 
 def pack(x: torch.Tensor, format: str = "int8") -> Packed:
     """x (CUDA, float32, bfloat16 or float16, any shape and strides) in 8 bits, in blocks of 32 along its elements in order."""
-    B._format(format)
-    x = x.detach().contiguous()
-    data = torch.empty(max(B.dn_packed_bytes(x.numel()), 1), dtype=torch.uint8, device=x.device)
-    if x.numel():
-        B.dn_pack(x, format, data)
+    data = B.native().packed(x, B._format(format))
+    if isinstance(data, int):
+        raise B.DnError(data, "dn_pack")
     return Packed(data, format, x.shape, x.dtype)
 
 

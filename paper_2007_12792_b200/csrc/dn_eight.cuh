@@ -14,6 +14,8 @@
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
 
+#include <type_traits>
+
 #include "dn_internal.cuh"
 
 namespace dn {
@@ -141,6 +143,11 @@ __device__ __forceinline__ void gates(const Cols<V>& z, Cols<V>& p, Cols<V>& q, 
 __device__ __forceinline__ unsigned magnitude_bits(float v) {
     const unsigned m = __float_as_uint(v) & 0x7fffffffu;
     return m < 0x7f800000u ? m : 0u;
+}
+// the biased exponent (255: not finite) of a value whose upper 16 bits without the sign these are
+template <class T> __device__ __forceinline__ int magnitude_exponent(uint32_t upper) {
+    if constexpr (std::is_same_v<T, __half>) return (int)(__float_as_uint(__half2float(__ushort_as_half((unsigned short)upper))) >> 23);
+    else return (int)(upper >> 7);
 }
 // the scale's byte (e + 127, 1 .. 248) for a block whose largest magnitude has these bits
 __device__ __forceinline__ int scale_byte(unsigned bits, bool int8) {

@@ -544,6 +544,52 @@ PyObject* unpack(PyObject*, PyObject* const* a, Py_ssize_t nargs) {            /
         return DN_NO_GIL(dn_unpack(t.numel(), type, p.data_ptr(), format, t.data_ptr(), st));
     });
 }
+PyObject* packed(PyObject*, PyObject* const* a, Py_ssize_t nargs) {            // src of any layout, format: the packed tensor, or a status
+    DN_ARGS(2);
+    HANDLE_TH_ERRORS
+    const at::Tensor& src = a_tensor(a[0], "src");
+    const int32_t type = type_code(src.scalar_type(), "src"), format = small_integer(a[1], "format");
+    Device d;
+    d.see(src, "src");
+    c10::cuda::CUDAGuard guard(*d.one);
+    at::Tensor out;
+    dn_status st = DN_OK;
+    {
+        pybind11::gil_scoped_release no_gil;
+        at::NoGradGuard no_grad;
+        const at::Tensor t = src.contiguous();
+        out = new_bytes(dn_packed_bytes(t.numel()), t);
+        if (t.numel() > 0) st = dn_pack(t.numel(), type, t.data_ptr(), format, out.data_ptr(), c10::cuda::getCurrentCUDAStream(d.one->index()).stream());
+    }
+    if (st != DN_OK) return PyLong_FromLong((long)st);
+    return THPVariable_Wrap(out);
+    END_HANDLE_TH_ERRORS
+}
+PyObject* unpacked(PyObject*, PyObject* const* a, Py_ssize_t nargs) {          // packed, format, shape, dtype: a new tensor, or a status
+    DN_ARGS(4);
+    HANDLE_TH_ERRORS
+    const at::Tensor& p = a_tensor(a[0], "packed");
+    const int32_t format = small_integer(a[1], "format");
+    TORCH_CHECK_TYPE(PyTuple_Check(a[2]) && THPDtype_Check(a[3]), "unpack: expected a shape and a dtype");
+    std::vector<int64_t> shape;
+    for (Py_ssize_t i = 0; i < PyTuple_GET_SIZE(a[2]); ++i) shape.push_back(integer(PyTuple_GET_ITEM(a[2], i), "shape"));
+    const at::ScalarType dtype = reinterpret_cast<THPDtype*>(a[3])->scalar_type;
+    const int32_t type = type_code(dtype, "dtype");
+    Device d;
+    bytes_checked(p, "packed", d);
+    c10::cuda::CUDAGuard guard(*d.one);
+    at::Tensor out;
+    dn_status st = DN_OK;
+    {
+        pybind11::gil_scoped_release no_gil;
+        out = at::empty(shape, p.options().dtype(dtype));
+        TORCH_CHECK_VALUE((size_t)p.numel() >= dn_packed_bytes(out.numel()), "packed: ", p.numel(), " bytes, expected ", dn_packed_bytes(out.numel()));
+        if (out.numel() > 0) st = dn_unpack(out.numel(), type, p.data_ptr(), format, out.data_ptr(), c10::cuda::getCurrentCUDAStream(d.one->index()).stream());
+    }
+    if (st != DN_OK) return PyLong_FromLong((long)st);
+    return THPVariable_Wrap(out);
+    END_HANDLE_TH_ERRORS
+}
 PyObject* activation_forward(PyObject*, PyObject* const* a, Py_ssize_t nargs) {          // kind, x, y, format, packed, stream
     DN_ARGS(6);
     return status([&]() {
@@ -579,6 +625,8 @@ PyMethodDef methods[] = {
     {"scan_backward", (PyCFunction)(void (*)(void))scan_backward, METH_FASTCALL, nullptr},
     {"gated_scan", (PyCFunction)(void (*)(void))gated_scan, METH_FASTCALL, nullptr},
     {"activation", (PyCFunction)(void (*)(void))activation, METH_FASTCALL, nullptr},
+    {"packed", (PyCFunction)(void (*)(void))packed, METH_FASTCALL, nullptr},
+    {"unpacked", (PyCFunction)(void (*)(void))unpacked, METH_FASTCALL, nullptr},
     {"pack", (PyCFunction)(void (*)(void))pack, METH_FASTCALL, nullptr},
     {"unpack", (PyCFunction)(void (*)(void))unpack, METH_FASTCALL, nullptr},
     {"activation_forward", (PyCFunction)(void (*)(void))activation_forward, METH_FASTCALL, nullptr},

@@ -9,54 +9,93 @@
 namespace dn {
 namespace {
 
-constexpr int SAVED_THREADS = 256, UNIT = 8, UNITS = 4;
+constexpr int SAVED_THREADS = 256, UNIT = 8, UNITS = 4, PAIRS = UNIT / 2;
 
 __host__ __device__ constexpr int64_t scales_at(int64_t n) { return (n + 15) / 16 * 16; }
 
-template <class T> __device__ __forceinline__ void load_unit(const T* p, int64_t i, int64_t n, bool wide, float (&f)[UNIT]) {
+using Pair = Cols<2>;
+template <class T> struct Unit { uint4 w[UNIT * sizeof(T) / 16]; };          // 8 values as they lie in memory
+
+template <class T> __device__ __forceinline__ Unit<T> load_unit(const T* p, int64_t i, int64_t n, bool wide) {
+    Unit<T> u;
     if (wide && i + UNIT <= n) {
-        T t[UNIT];
-        constexpr int W = UNIT * sizeof(T) / 16;
-        uint4 r[W];
 #pragma unroll
-        for (int k = 0; k < W; ++k) r[k] = reinterpret_cast<const uint4*>(p + i)[k];
-        memcpy(t, r, sizeof t);
-#pragma unroll
-        for (int j = 0; j < UNIT; ++j) f[j] = as_float(t[j]);
+        for (int k = 0; k < (int)(UNIT * sizeof(T) / 16); ++k) u.w[k] = reinterpret_cast<const uint4*>(p + i)[k];
     } else {
-#pragma unroll
-        for (int j = 0; j < UNIT; ++j) f[j] = i + j < n ? as_float(p[i + j]) : 0.0f;
-    }
-}
-template <class T> __device__ __forceinline__ void store_unit(T* p, int64_t i, int64_t n, bool wide, const float (&f)[UNIT]) {
-    if (wide && i + UNIT <= n) {
         T t[UNIT];
-        constexpr int W = UNIT * sizeof(T) / 16;
-        uint4 r[W];
 #pragma unroll
-        for (int j = 0; j < UNIT; ++j) t[j] = rounded<T>(f[j]);
-        memcpy(r, t, sizeof t);
+        for (int j = 0; j < UNIT; ++j) t[j] = i + j < n ? p[i + j] : rounded<T>(0.0f);
+        memcpy(&u, t, sizeof u);
+    }
+    return u;
+}
+template <class T> __device__ __forceinline__ void values_in(const Unit<T>& u, Pair (&f)[PAIRS]) {
+    T t[UNIT];
+    memcpy(t, &u, sizeof t);
 #pragma unroll
-        for (int k = 0; k < W; ++k) reinterpret_cast<uint4*>(p + i)[k] = r[k];
+    for (int j = 0; j < PAIRS; ++j) f[j] = Pair{{as_float(t[2 * j]), as_float(t[2 * j + 1])}};
+}
+template <class T> __device__ __forceinline__ void store_unit(T* p, int64_t i, int64_t n, bool wide, const Pair (&f)[PAIRS]) {
+    T t[UNIT];
+#pragma unroll
+    for (int j = 0; j < UNIT; ++j) t[j] = rounded<T>(f[j / 2].v[j % 2]);
+    if (wide && i + UNIT <= n) {
+        Unit<T> u;
+        memcpy(&u, t, sizeof u);
+#pragma unroll
+        for (int k = 0; k < (int)(UNIT * sizeof(T) / 16); ++k) reinterpret_cast<uint4*>(p + i)[k] = u.w[k];
     } else {
 #pragma unroll
         for (int j = 0; j < UNIT; ++j)
-            if (i + j < n) p[i + j] = rounded<T>(f[j]);
+            if (i + j < n) p[i + j] = t[j];
+    }
+}
+
+// The exponent (biased; 255: not finite) of the largest magnitude of a block, from the four lanes that hold it.  Of 16-bit values two
+// are compared at a time, as integers without their signs.
+template <class T> __device__ __forceinline__ int largest_exponent(const Unit<T>& u) {
+    if constexpr (sizeof(T) == 4) {
+        unsigned m = 0;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) m = max(max(m, max(u.w[k].x & 0x7fffffffu, u.w[k].y & 0x7fffffffu)), max(u.w[k].z & 0x7fffffffu, u.w[k].w & 0x7fffffffu));
+        m = max(m, __shfl_xor_sync(~0u, m, 1));
+        m = max(m, __shfl_xor_sync(~0u, m, 2));
+        return (int)(m >> 23);
+    } else {
+        unsigned m = __vmaxu2(__vmaxu2(u.w[0].x & 0x7fff7fffu, u.w[0].y & 0x7fff7fffu), __vmaxu2(u.w[0].z & 0x7fff7fffu, u.w[0].w & 0x7fff7fffu));
+        m = __vmaxu2(m, __shfl_xor_sync(~0u, m, 1));
+        m = __vmaxu2(m, __shfl_xor_sync(~0u, m, 2));
+        return magnitude_exponent<T>(max(m & 0xffffu, m >> 16));
     }
 }
 
 // the codes and the scale of a block, from the four lanes that hold it (each warp calls this as a whole)
-__device__ __forceinline__ void store_codes(uint8_t* packed, int64_t i, int64_t n, bool int8, const float (&f)[UNIT]) {
-    unsigned m = 0;
-#pragma unroll
-    for (int j = 0; j < UNIT; ++j) m = max(m, magnitude_bits(f[j]));
-    m = max(m, __shfl_xor_sync(~0u, m, 1));
-    m = max(m, __shfl_xor_sync(~0u, m, 2));
-    const int byte = scale_byte(m, int8);
-    const float inverse = inverse_scale_of(byte);
+template <class T> __device__ __forceinline__ void store_codes(uint8_t* packed, int64_t i, int64_t n, bool int8, const Unit<T>& u, const Pair (&f)[PAIRS]) {
+    const int e = largest_exponent(u);
     uint32_t c[2] = {};
+    int byte = max(e - (int8 ? 6 : 7), 1);
+    if (__any_sync(~0u, e == 255)) {                       // values that are not finite
+        unsigned m = 0;
 #pragma unroll
-    for (int j = 0; j < UNIT; ++j) c[j / 4] |= code8(f[j], inverse, int8) << (8 * (j % 4));
+        for (int j = 0; j < UNIT; ++j) m = max(m, magnitude_bits(f[j / 2].v[j % 2]));
+        m = max(m, __shfl_xor_sync(~0u, m, 1));
+        m = max(m, __shfl_xor_sync(~0u, m, 2));
+        byte = scale_byte(m, int8);
+#pragma unroll
+        for (int j = 0; j < UNIT; ++j) c[j / 4] |= code8(f[j / 2].v[j % 2], inverse_scale_of(byte), int8) << (8 * (j % 4));
+    } else {
+        const float inverse = inverse_scale_of(byte);
+        uint32_t k[PAIRS];
+        if (int8) {
+#pragma unroll
+            for (int j = 0; j < PAIRS; ++j) k[j] = codes_int8(f[j], inverse);
+        } else {
+#pragma unroll
+            for (int j = 0; j < PAIRS; ++j) k[j] = codes_e4m3(f[j], inverse);
+        }
+        c[0] = __byte_perm(k[0], k[1], 0x5410);
+        c[1] = __byte_perm(k[2], k[3], 0x5410);
+    }
     if (i + UNIT <= n) {
         *reinterpret_cast<uint2*>(packed + i) = make_uint2(c[0], c[1]);
     } else {
@@ -75,52 +114,102 @@ __device__ __forceinline__ Codes load_codes(const uint8_t* packed, int64_t i, in
         r.c[1] = u.y;
     } else {
 #pragma unroll
-        for (int j = 0; j < UNIT; ++j)
-            if (i + j < n) r.c[j / 4] |= (uint32_t)packed[i + j] << (8 * (j % 4));
+        for (int j = 0; j < UNIT; ++j) r.c[j / 4] |= (i + j < n ? (uint32_t)packed[i + j] : 128u) << (8 * (j % 4));
     }
     if (i < n) r.byte = packed[scales_at(n) + i / kBlock8];
     return r;
 }
-__device__ __forceinline__ void values_of(const Codes& r, bool int8, float (&f)[UNIT]) {
+__device__ __forceinline__ void values_of(const Codes& r, bool int8, Pair (&f)[PAIRS]) {
     const float scale = scale_of(r.byte);
+    if (int8) {
 #pragma unroll
-    for (int j = 0; j < UNIT; ++j) f[j] = value8((r.c[j / 4] >> (8 * (j % 4))) & 255, scale, int8);
+        for (int j = 0; j < PAIRS; ++j) f[j] = values_int8<2>(r.c[j / 2] >> (16 * (j % 2)), scale);
+        if (any_zero_byte(r.c[0]) | any_zero_byte(r.c[1])) {
+#pragma unroll
+            for (int j = 0; j < UNIT; ++j)
+                if (((r.c[j / 4] >> (8 * (j % 4))) & 255) == 0) f[j / 2].v[j % 2] = __uint_as_float(0x7fffffffu);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < PAIRS; ++j) f[j] = values_e4m3<2>((r.c[j / 2] >> (16 * (j % 2))) & 0xffff, scale);
+    }
 }
 
 // z of the gate s(z) and dz/dx; beyond |x| = 16 the gate is 0 or 1 to the last bit and x^3 could overflow
-template <int KIND> __device__ __forceinline__ float gate_argument(float x, float& dz) {
-    if (KIND == DN_SILU) { dz = 1.0f; return x; }
-    constexpr float two_c = 1.5957691216057308f;           // 2 sqrt(2 / pi)
-    const float t = fabsf(x) > 16.0f ? copysignf(16.0f, x) : x, t2 = t * t;
-    dz = two_c * fmaf(3.0f * 0.044715f, t2, 1.0f);
-    return two_c * t * fmaf(0.044715f, t2, 1.0f);
+__device__ __forceinline__ Pair held16(const Pair& x) {
+    Pair t = x;
+#pragma unroll
+    for (int v = 0; v < 2; ++v)
+        if (fabsf(x.v[v]) > 16.0f) t.v[v] = copysignf(16.0f, x.v[v]);
+    return t;
 }
-template <int KIND, bool ACCURATE> __device__ __forceinline__ float activation(float x) {
-    if (KIND == DN_TANH) return tanhf(x);
-    float dz, p, q;
-    two_sided_gates<ACCURATE>(gate_argument<KIND>(x, dz), p, q);
-    return x * p;
-}
-template <int KIND, bool ACCURATE> __device__ __forceinline__ float slope(float x) {
-    float dz, p, q;
-    if (KIND == DN_TANH) {                                 // 1 - tanh^2 = 4 s(2x) s(-2x), which keeps its digits where tanh is near 1
-        two_sided_gates<ACCURATE>(2.0f * x, p, q);
-        return 4.0f * p * q;
+constexpr float TWO_C = 1.5957691216057308f;               // 2 sqrt(2 / pi)
+// s(z) and s(-z) of a pair.  With 16-bit results e^-|z| is the square of an approximate exponential of half the argument: the product is
+// also right below the smallest normal number, where z multiplies s(z) back up into the type's range.
+template <bool ACCURATE> __device__ __forceinline__ void pair_gates(const Pair& z, Pair& p, Pair& q) {
+    if constexpr (ACCURATE) {
+#pragma unroll
+        for (int v = 0; v < 2; ++v) two_sided_gates<true>(z.v[v], p.v[v], q.v[v]);
+    } else {
+        const Pair t = mul(z, all_of<2>(0.7213475204444817f));       // log2 e / 2
+        Pair e, r;
+#pragma unroll
+        for (int v = 0; v < 2; ++v) exponential_gate(-fabsf(t.v[v]), e.v[v]);
+        e = mul(e, e);
+        const Pair d = add(e, all_of<2>(1.0f));
+#pragma unroll
+        for (int v = 0; v < 2; ++v) reciprocal_gate(d.v[v], r.v[v]);
+        const Pair less = mul(e, r);
+#pragma unroll
+        for (int v = 0; v < 2; ++v) {
+            p.v[v] = z.v[v] >= 0.0f ? r.v[v] : less.v[v];
+            q.v[v] = z.v[v] >= 0.0f ? less.v[v] : r.v[v];
+        }
     }
-    const float z = gate_argument<KIND>(x, dz);
-    two_sided_gates<ACCURATE>(z, p, q);
-    if (KIND == DN_GELU) x = fabsf(x) > 16.0f ? copysignf(16.0f, x) : x;
-    return p * fmaf(x * q, dz, 1.0f);
+}
+template <int KIND, bool ACCURATE> __device__ __forceinline__ Pair activation(const Pair& x) {
+    if constexpr (KIND == DN_TANH) return Pair{{tanhf(x.v[0]), tanhf(x.v[1])}};
+    else {
+        Pair p, q, z = x;
+        if constexpr (KIND == DN_GELU) {
+            const Pair t = held16(x);
+            z = mul(mul(t, all_of<2>(TWO_C)), fma(mul(t, t), all_of<2>(0.044715f), all_of<2>(1.0f)));
+        }
+        pair_gates<ACCURATE>(z, p, q);
+        return mul(x, p);
+    }
+}
+template <int KIND, bool ACCURATE> __device__ __forceinline__ Pair slope(Pair x) {
+    Pair p, q;
+    if constexpr (KIND == DN_TANH) {                       // 1 - tanh^2 = 4 s(2x) s(-2x), which keeps its digits where tanh is near 1
+#pragma unroll
+        for (int v = 0; v < 2; ++v) two_sided_gates<ACCURATE>(2.0f * x.v[v], p.v[v], q.v[v]);
+        return mul(mul(p, all_of<2>(4.0f)), q);
+    } else if constexpr (KIND == DN_SILU) {
+        pair_gates<ACCURATE>(x, p, q);
+        return fma(mul(x, q), p, p);
+    } else {
+        x = held16(x);
+        const Pair x2 = mul(x, x);
+        const Pair z = mul(mul(x, all_of<2>(TWO_C)), fma(x2, all_of<2>(0.044715f), all_of<2>(1.0f)));
+        const Pair dz = fma(x2, all_of<2>(TWO_C * 3.0f * 0.044715f), all_of<2>(TWO_C));
+        pair_gates<ACCURATE>(z, p, q);
+        return fma(mul(mul(x, q), dz), p, p);
+    }
 }
 
 template <class T> __global__ void __launch_bounds__(SAVED_THREADS) pack_kernel(int64_t n, const T* src, int int8, uint8_t* packed, bool wide) {
     dep_wait();
     const int64_t first = ((int64_t)blockIdx.x * SAVED_THREADS * UNITS + threadIdx.x) * UNIT;
-    float f[UNITS][UNIT];
+    Unit<T> w[UNITS];
 #pragma unroll
-    for (int u = 0; u < UNITS; ++u) load_unit(src, first + (int64_t)u * SAVED_THREADS * UNIT, n, wide, f[u]);
+    for (int u = 0; u < UNITS; ++u) w[u] = load_unit(src, first + (int64_t)u * SAVED_THREADS * UNIT, n, wide);
 #pragma unroll
-    for (int u = 0; u < UNITS; ++u) store_codes(packed, first + (int64_t)u * SAVED_THREADS * UNIT, n, int8, f[u]);
+    for (int u = 0; u < UNITS; ++u) {
+        Pair f[PAIRS];
+        values_in(w[u], f);
+        store_codes(packed, first + (int64_t)u * SAVED_THREADS * UNIT, n, int8, w[u], f);
+    }
 }
 template <class T> __global__ void __launch_bounds__(SAVED_THREADS) unpack_kernel(int64_t n, T* dst, int int8, const uint8_t* packed, bool wide) {
     dep_wait();
@@ -130,7 +219,7 @@ template <class T> __global__ void __launch_bounds__(SAVED_THREADS) unpack_kerne
     for (int u = 0; u < UNITS; ++u) r[u] = load_codes(packed, first + (int64_t)u * SAVED_THREADS * UNIT, n);
 #pragma unroll
     for (int u = 0; u < UNITS; ++u) {
-        float f[UNIT];
+        Pair f[PAIRS];
         values_of(r[u], int8, f);
         store_unit(dst, first + (int64_t)u * SAVED_THREADS * UNIT, n, wide, f);
     }
@@ -139,36 +228,39 @@ template <class T, int KIND>
 __global__ void __launch_bounds__(SAVED_THREADS) activation_forward_kernel(int64_t n, const T* x, T* y, int int8, uint8_t* packed, bool wide) {
     dep_wait();
     const int64_t first = ((int64_t)blockIdx.x * SAVED_THREADS * UNITS + threadIdx.x) * UNIT;
-    float f[UNITS][UNIT];
+    Unit<T> w[UNITS];
 #pragma unroll
-    for (int u = 0; u < UNITS; ++u) load_unit(x, first + (int64_t)u * SAVED_THREADS * UNIT, n, wide, f[u]);
+    for (int u = 0; u < UNITS; ++u) w[u] = load_unit(x, first + (int64_t)u * SAVED_THREADS * UNIT, n, wide);
 #pragma unroll
     for (int u = 0; u < UNITS; ++u) {
         const int64_t i = first + (int64_t)u * SAVED_THREADS * UNIT;
-        if (packed) store_codes(packed, i, n, int8, f[u]);
+        Pair f[PAIRS];
+        values_in(w[u], f);
+        if (packed) store_codes(packed, i, n, int8, w[u], f);
 #pragma unroll
-        for (int j = 0; j < UNIT; ++j) f[u][j] = activation<KIND, sizeof(T) == 4>(f[u][j]);
-        store_unit(y, i, n, wide, f[u]);
+        for (int j = 0; j < PAIRS; ++j) f[j] = activation<KIND, sizeof(T) == 4>(f[j]);
+        store_unit(y, i, n, wide, f);
     }
 }
 template <class T, int KIND>
 __global__ void __launch_bounds__(SAVED_THREADS) activation_backward_kernel(int64_t n, const uint8_t* packed, int int8, const T* dy, T* dx, bool wide) {
     dep_wait();
     const int64_t first = ((int64_t)blockIdx.x * SAVED_THREADS * UNITS + threadIdx.x) * UNIT;
-    float d[UNITS][UNIT];
+    Unit<T> w[UNITS];
     Codes r[UNITS];
 #pragma unroll
     for (int u = 0; u < UNITS; ++u) {
-        load_unit(dy, first + (int64_t)u * SAVED_THREADS * UNIT, n, wide, d[u]);
+        w[u] = load_unit(dy, first + (int64_t)u * SAVED_THREADS * UNIT, n, wide);
         r[u] = load_codes(packed, first + (int64_t)u * SAVED_THREADS * UNIT, n);
     }
 #pragma unroll
     for (int u = 0; u < UNITS; ++u) {
-        float f[UNIT];
+        Pair f[PAIRS], d[PAIRS];
         values_of(r[u], int8, f);
+        values_in(w[u], d);
 #pragma unroll
-        for (int j = 0; j < UNIT; ++j) d[u][j] *= slope<KIND, sizeof(T) == 4>(f[j]);
-        store_unit(dx, first + (int64_t)u * SAVED_THREADS * UNIT, n, wide, d[u]);
+        for (int j = 0; j < PAIRS; ++j) d[j] = mul(d[j], slope<KIND, sizeof(T) == 4>(f[j]));
+        store_unit(dx, first + (int64_t)u * SAVED_THREADS * UNIT, n, wide, d);
     }
 }
 

@@ -139,11 +139,6 @@ template <class T, int V> __device__ __forceinline__ uint32_t magnitudes(Raw<T, 
     else if constexpr (V == 1) return (g | (uint32_t)x << 16) & 0x7fff7fffu;
     else return __vmaxu2(__byte_perm(g, x, 0x5410) & 0x7fff7fffu, __byte_perm(g, x, 0x7632) & 0x7fff7fffu);
 }
-template <class T> __device__ __forceinline__ int exponent_of(uint32_t magnitude) {          // biased; 255: not finite
-    if constexpr (std::is_same_v<T, __half>) return (int)(__float_as_uint(__half2float(__ushort_as_half((unsigned short)magnitude))) >> 23);
-    else return (int)(magnitude >> 7);
-}
-
 // Per block: where it stands, and what a step of it exchanges.  The blocks of a cluster send one another the map of their tile; a buffer
 // is written again two steps later, when its readers have sent what they found with it.
 template <int V, int LX, int WR, int WC, int R> struct Exchange {
@@ -287,7 +282,7 @@ __global__ void __launch_bounds__(32 * WR * WC, SAVE8 ? 3 : 4) scan_forward_kern
                 m[j] = __vmaxu2(keep, __shfl_xor_sync(~0u, send, h));
             }
         if (V == 1) m[0] = __vmaxu2(m[0], __shfl_xor_sync(~0u, m[0], 16));
-        const int eg = exponent_of<T>(m[0] & 0xffffu), exx = exponent_of<T>(m[0] >> 16);
+        const int eg = magnitude_exponent<T>(m[0] & 0xffffu), exx = magnitude_exponent<T>(m[0] >> 16);
         const int block = at.first / kBlock8 + (threadIdx.x >> 5) / WR * V + (V == 2 ? lane >> 4 : 0);
         uint8_t *const gs = A.gs + ((int64_t)at.b * A.nblk + block) * A.rows_padded + t0, *const xs = A.xs + ((int64_t)at.b * A.nblk + block) * A.rows_padded + t0;
         const bool mine = block < A.nblk && t0 < A.rows_padded;
