@@ -11,7 +11,7 @@
 // states are formed again from one in 32 bits ahead of every 64 rows) and M (mu from zero).
 #include "dn_eight.cuh"
 
-#include <type_traits>
+#include <cuda.h>
 
 namespace dn {
 namespace {
@@ -100,6 +100,24 @@ __device__ __forceinline__ bool barrier_wait(uint64_t* bar, unsigned parity) {
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
+// ---- bulk copies of tiles (coordinates: column, row, sample) ----
+struct TileMaps { CUtensorMap in[3], out[4]; };            // g, x, dh; h or dg, dx, codes of g, codes of x
+__device__ __forceinline__ void tile_load(void* to, const CUtensorMap& m, int col, int row, int b, uint64_t* bar) {
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
+                     (unsigned)__cvta_generic_to_shared(to)), "l"(&m), "r"(col), "r"(row), "r"(b), "r"((unsigned)__cvta_generic_to_shared(bar)) : "memory");
+}
+__device__ __forceinline__ void tile_store(const CUtensorMap& m, const void* from, int col, int row, int b) {
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(&m),
+                 "r"((unsigned)__cvta_generic_to_shared(from)), "r"(col), "r"(row), "r"(b) : "memory");
+}
+__device__ __forceinline__ void stores_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void stores_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }   // their shared memory may be written again
+__device__ __forceinline__ void stores_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+__device__ __forceinline__ unsigned char* on_128(unsigned char* shared) {         // the next multiple of 128 bytes
+    return shared + (-(unsigned)__cvta_generic_to_shared(shared) & 127u);
+}
+__device__ __forceinline__ void shared_to_bulk() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
 // factors and offsets of V adjacent columns, in one access
 template <int V> struct __align__(8 * V) Maps { Cols<V> p, h; };
 
@@ -145,7 +163,6 @@ template <int V, int LX, int WR, int WC, int R> struct Exchange {
     using Pl = Place<V, LX, WR, WC, R>;
     static constexpr int NG = Pl::NG, LANES = WC * LX;
     Maps<V> agg[2][NG > 1 ? NG : 1][NG > 1 ? LANES : 1];
-    Maps<V> tot[2][SCAN_MOST_BLOCKS][NG > 1 ? LANES : 1];
     uint64_t bars[2];
 
     __device__ void init(int K) {
@@ -157,8 +174,8 @@ template <int V, int LX, int WR, int WC, int R> struct Exchange {
     }
     // The value that enters this thread's rows, from the map (p, h) of these rows and the value `carry` that enters the step's first ones;
     // carry becomes what leaves the last ones.  DOWN: rows are passed from the last to the first.  `between`: what to do once all maps of
-    // the block can be read.
-    template <bool DOWN, class F> __device__ __forceinline__ Cols<V> enter(int k, int K, int rank, int q, int lane, const Cols<V>& p, const Cols<V>& h, Cols<V>& carry, bool& lost, F between) {
+    // the block can be read.  sent: what the blocks of the cluster sent, [2][K][LANES].
+    template <bool DOWN, class F> __device__ __forceinline__ Cols<V> enter(Maps<V>* sent, int k, int K, int rank, int q, int lane, const Cols<V>& p, const Cols<V>& h, Cols<V>& carry, bool& lost, F between) {
         if constexpr (NG == 1) {
             const Cols<V> in = carry;
             carry = fma(p, carry, h);
@@ -190,7 +207,7 @@ template <int V, int LX, int WR, int WC, int R> struct Exchange {
                 else { ht = fma(e.p, ht, e.h); pt = mul(e.p, pt); }
             }
             for (int peer = q; peer < K; peer += NG) {
-                const unsigned to = cluster_address(&tot[buf][rank][lane], peer), bar = cluster_address(&bars[buf], peer);
+                const unsigned to = cluster_address(&sent[(buf * K + rank) * LANES + lane], peer), bar = cluster_address(&bars[buf], peer);
                 if constexpr (V == 1) cluster_send(to, bar, pt.v[0], ht.v[0]); else cluster_send(to, bar, pt.v[0], pt.v[1], ht.v[0], ht.v[1]);
             }
             if (threadIdx.x == 0) barrier_expect(&bars[buf], K * LANES * (unsigned)sizeof(Maps<V>));
@@ -198,13 +215,13 @@ template <int V, int LX, int WR, int WC, int R> struct Exchange {
             const int ahead = DOWN ? K - 1 - rank : rank;
 #pragma unroll 4
             for (int i = 0; i < ahead; ++i) {
-                const Maps<V> e = tot[buf][DOWN ? K - 1 - i : i][lane];
+                const Maps<V> e = sent[(buf * K + (DOWN ? K - 1 - i : i)) * LANES + lane];
                 carry = fma(e.p, carry, e.h);
             }
             in = fma(pb, carry, hb);
 #pragma unroll 4
             for (int i = ahead; i < K; ++i) {
-                const Maps<V> e = tot[buf][DOWN ? K - 1 - i : i][lane];
+                const Maps<V> e = sent[(buf * K + (DOWN ? K - 1 - i : i)) * LANES + lane];
                 carry = fma(e.p, carry, e.h);
             }
             if (lost) in = carry = all_of<V>(__uint_as_float(0x7fffffffu));
@@ -214,18 +231,45 @@ template <int V, int LX, int WR, int WC, int R> struct Exchange {
 };
 
 // ---- forward -----------------------------------------------------------------------------------------------------------------
-template <class T, int V, int LX, int WR, int WC, int R, bool SAVE8, bool MIX, class Off>
-__global__ void __launch_bounds__(32 * WR * WC, SAVE8 ? 3 : 4) scan_forward_kernel(const __grid_constant__ ScanArgs A) {
+constexpr int FORWARD_STAGES = 2, BACKWARD_STAGES = 2;     // tiles of a block that are on their way or being read
+
+// Shared memory of a block that moves its tiles by bulk copies: IN input tiles per stage, and per warp a piece of each output.
+template <int STAGES, int IN_BYTES, int WARPS, int OUT_BYTES> struct __align__(128) Tiles {
+    unsigned char in[STAGES][IN_BYTES];
+    unsigned char out[WARPS][OUT_BYTES];
+    uint64_t arrived[STAGES];
+};
+template <class T, int V, bool SAVE8> using ForwardTiles =
+    Tiles<FORWARD_STAGES, 2 * 64 * 32 * V * (int)sizeof(T), 4, 16 * 32 * V * ((int)sizeof(T) + (SAVE8 ? 2 : 0))>;
+template <class T, int V, bool SAVED8> using BackwardTiles =
+    Tiles<BACKWARD_STAGES, 64 * 32 * V * (SAVED8 ? (int)sizeof(T) + 2 : 3 * (int)sizeof(T)), 8, 8 * 32 * V * 2 * (int)sizeof(T)>;
+
+template <class T, int V, int LX, int WR, int WC, int R, bool SAVE8, bool MIX, bool BULK, class Off>
+__global__ void __launch_bounds__(32 * WR * WC, SAVE8 ? 3 : 4) scan_forward_kernel(const __grid_constant__ ScanArgs A, const __grid_constant__ TileMaps maps) {
+    static_assert(!BULK || (LX == 32 && WR == 4 && WC == 1 && R == 16), "the tiles and pieces of the tensor maps");
     static_assert(!SAVE8 || (LX == 32 && R == 16), "a row's 32 columns of a scale lie in one warp, 16 rows' scales in 16 lanes");
     using Pl = Place<V, LX, WR, WC, R>;
     using W = Raw<T, V>;
     constexpr int NG = Pl::NG, TILE = Pl::TILE, S = sizeof(T);
+    constexpr int ROW = 32 * V * S, ST = FORWARD_STAGES;   // bytes of a tile's row
     __shared__ Exchange<V, LX, WR, WC, R> ex;
+    extern __shared__ __align__(128) unsigned char dynamic[];
+    using Here = ForwardTiles<T, V, SAVE8>;
+    [[maybe_unused]] Here& tiles = *reinterpret_cast<Here*>(on_128(dynamic));
+    auto* const sent = reinterpret_cast<Maps<V>*>(BULK ? on_128(dynamic) + sizeof(Here) : dynamic);
     Pl at(A);
     const int q = at.q, c = at.c;
     const bool cv = at.cv;
     const int K = NG > 1 ? A.blocks : 1;
     ex.init(K);
+    if constexpr (BULK) {
+        if (threadIdx.x == 0) {
+#pragma unroll
+            for (int i = 0; i < ST; ++i) barrier_init(&tiles.arrived[i]);
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        }
+        __syncthreads();
+    }
     bool lost = false;
     const float none = S == 4 ? 0.0f : least_decay();
     dep_wait();
@@ -261,8 +305,30 @@ __global__ void __launch_bounds__(32 * WR * WC, SAVE8 ? 3 : 4) scan_forward_kern
             }
         }
     };
-    if (steps > 0) fetch(row0);
+    [[maybe_unused]] auto order = [&](int s) {             // one thread: the tile of step s
+        uint64_t* bar = &tiles.arrived[s % ST];
+        unsigned char* to = tiles.in[s % ST];
+        const int row = (s * K + at.rank) * TILE;
+        barrier_expect(bar, 2 * TILE * ROW);
+        tile_load(to, maps.in[0], at.first, row, at.b, bar);
+        tile_load(to + TILE * ROW, maps.in[1], at.first, row, at.b, bar);
+    };
+    [[maybe_unused]] auto take = [&](int s) {              // this thread's part of it
+        lost = !barrier_wait(&tiles.arrived[s % ST], (s / ST) & 1) || lost;
+        const unsigned char* from = tiles.in[s % ST] + q * R * ROW + at.col * S;
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            rg[i] = *reinterpret_cast<const W*>(from + i * ROW);
+            rx[i] = *reinterpret_cast<const W*>(from + TILE * ROW + i * ROW);
+        }
+    };
+    if constexpr (BULK) {
+        if (threadIdx.x == 0)
+            for (int s = 0; s < ST && s < steps; ++s) order(s);
+    } else if (steps > 0) fetch(row0);
     if (K > 1) { cluster_arrive(); cluster_wait(); }       // every block of the cluster runs before one writes to another
+    [[maybe_unused]] unsigned char* const mine_out = BULK ? tiles.out[threadIdx.x >> 5] + at.col * S : nullptr;
+    [[maybe_unused]] unsigned char* const mine_codes = BULK ? tiles.out[threadIdx.x >> 5] + R * ROW + at.col : nullptr;
 
     // Codes and scales of this warp's 16 rows.  The largest magnitudes of the 16 rows are found together: at every stage of a butterfly a lane
     // hands half of its rows to the other and keeps the other's share of the rest, 15 exchanges of gate and input at once in place of 64
@@ -288,6 +354,16 @@ __global__ void __launch_bounds__(32 * WR * WC, SAVE8 ? 3 : 4) scan_forward_kern
         const bool mine = block < A.nblk && t0 < A.rows_padded;
         uint8_t *const gq = A.gq + (((int64_t)at.b * A.rows + row0) * A.cols + at.first), *const xq = A.xq + (((int64_t)at.b * A.rows + row0) * A.cols + at.first);
         const Off oq = (Off)(q * R) * (Off)A.cols + (Off)at.col;
+        auto put = [&](int i, uint32_t kg, uint32_t kx) {
+            using Q = std::conditional_t<V == 2, uint16_t, uint8_t>;
+            if constexpr (BULK) {
+                *reinterpret_cast<Q*>(mine_codes + i * 32 * V) = (Q)kg;
+                *reinterpret_cast<Q*>(mine_codes + (R + i) * 32 * V) = (Q)kx;
+            } else if (FULL || i < n) {
+                *reinterpret_cast<Q*>(gq + (int64_t)i * A.cols + oq) = (Q)kg;
+                *reinterpret_cast<Q*>(xq + (int64_t)i * A.cols + oq) = (Q)kx;
+            }
+        };
         if (__any_sync(~0u, eg == 255 || exx == 255)) {    // values that are not finite: row by row
             const char *g = bg + row0 * A.g.row, *x = bx + row0 * A.x.row;
 #pragma unroll 1
@@ -299,12 +375,13 @@ __global__ void __launch_bounds__(32 * WR * WC, SAVE8 ? 3 : 4) scan_forward_kern
 #pragma unroll
                 for (int h = V == 2 ? 8 : 16; h >= 1; h /= 2) { mg = max(mg, __shfl_xor_sync(~0u, mg, h)); mx = max(mx, __shfl_xor_sync(~0u, mx, h)); }
                 const int sg = scale_byte(mg, true), sx = scale_byte(mx, A.int8);
+                uint32_t kg = 0, kx = 0;
 #pragma unroll
-                for (int v = 0; v < V; ++v)
-                    if (i < n) {
-                        gq[(int64_t)i * A.cols + oq + v] = (uint8_t)code_int8(vg.v[v], inverse_scale_of(sg));
-                        xq[(int64_t)i * A.cols + oq + v] = (uint8_t)code8(vx.v[v], inverse_scale_of(sx), A.int8);
-                    }
+                for (int v = 0; v < V; ++v) {
+                    kg |= code_int8(vg.v[v], inverse_scale_of(sg)) << (8 * v);
+                    kx |= code8(vx.v[v], inverse_scale_of(sx), A.int8) << (8 * v);
+                }
+                put(i, kg, kx);
                 if (mine && (lane & (V == 2 ? 15 : 31)) == 0) { gs[i] = (uint8_t)sg; xs[i] = (uint8_t)sx; }
             }
             return;
@@ -318,12 +395,7 @@ __global__ void __launch_bounds__(32 * WR * WC, SAVE8 ? 3 : 4) scan_forward_kern
             const uint32_t kg = codes_int8(expand<T, V>(rg[i]), __uint_as_float(both << 16));
             const Cols<V> vx = expand<T, V>(rx[i]);
             const float ix = __uint_as_float(both & 0xffff0000u);
-            const uint32_t kx = A.int8 ? codes_int8(vx, ix) : codes_e4m3(vx, ix);
-            if (FULL || i < n) {
-                using Q = std::conditional_t<V == 2, uint16_t, uint8_t>;
-                *reinterpret_cast<Q*>(gq + (int64_t)i * A.cols + oq) = (Q)kg;
-                *reinterpret_cast<Q*>(xq + (int64_t)i * A.cols + oq) = (Q)kx;
-            }
+            put(i, kg, A.int8 ? codes_int8(vx, ix) : codes_e4m3(vx, ix));
         }
     };
 
@@ -347,17 +419,43 @@ __global__ void __launch_bounds__(32 * WR * WC, SAVE8 ? 3 : 4) scan_forward_kern
     for (int s = 0; s < steps; ++s) {
         const bool full = at.all && row0 + TILE <= len;
         const int t0 = row0 + q * R, n = cv ? len - t0 : 0;
+        if constexpr (BULK) {
+            take(s);
+            if ((threadIdx.x & 31) == 0) stores_read();    // the pieces of the step before
+            __syncwarp();
+        }
         if (full) prepare(Yes{}, n); else prepare(No{}, n);
-        if (s + 1 < steps) fetch(row0 + span);             // in flight while the states of this step are found
+        if constexpr (!BULK)
+            if (s + 1 < steps) fetch(row0 + span);         // in flight while the states of this step are found
 
-        Cols<V> hin = ex.template enter<false>(s, K, at.rank, q, at.col / V, P, H, carry, lost, [] {});
+        Cols<V> hin = ex.template enter<false>(sent, s, K, at.rank, q, at.col / V, P, H, carry, lost, [&] {
+            if constexpr (BULK)
+                if (threadIdx.x == 0 && s + ST < steps) order(s + ST);          // the block has read this step's tile
+        });
         if (A.states && cv && t0 % kChunkRows == 0 && t0 < A.rows) {
             float* st = A.states + ((int64_t)at.b * A.nchunk + t0 / kChunkRows) * A.cols + c;
 #pragma unroll
             for (int v = 0; v < V; ++v) st[v] = hin.v[v];
         }
         char* ph = bh + row0 * A.h.row;
-        if (full) {
+        if constexpr (BULK) {
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                hin = fma(a[i], hin, bb[i]);
+                *reinterpret_cast<W*>(mine_out + i * ROW) = full || i < n ? join<T, V>(hin) : W(0);
+            }
+            shared_to_bulk();
+            __syncwarp();
+            if ((threadIdx.x & 31) == 0 && t0 < A.rows) {
+                const unsigned char* from = tiles.out[threadIdx.x >> 5];
+                tile_store(maps.out[0], from, at.first, t0, at.b);
+                if (SAVE8) {
+                    tile_store(maps.out[2], from + R * ROW, at.first, t0, at.b);
+                    tile_store(maps.out[3], from + R * ROW + R * 32 * V, at.first, t0, at.b);
+                }
+                stores_commit();
+            }
+        } else if (full) {
 #pragma unroll
             for (int i = 0; i < R; ++i) {
                 hin = fma(a[i], hin, bb[i]);
@@ -380,13 +478,15 @@ __global__ void __launch_bounds__(32 * WR * WC, SAVE8 ? 3 : 4) scan_forward_kern
 #pragma unroll
         for (int v = 0; v < V; ++v) A.end[(int64_t)at.b * A.cols + c + v] = carry.v[v];
     }
+    if (BULK && (threadIdx.x & 31) == 0) stores_done();
     if (K > 1) { cluster_arrive(); cluster_wait(); }       // no block's shared memory goes while another could write to it
 }
 
 // ---- backward ----------------------------------------------------------------------------------------------------------------
-template <class T, int V, int LX, int WR, int WC, bool SAVED8, bool MIX, class Off>
-__global__ void __launch_bounds__(32 * WR * WC, 16 / (WR * WC)) scan_backward_kernel(const __grid_constant__ ScanArgs A) {
+template <class T, int V, int LX, int WR, int WC, bool SAVED8, bool MIX, bool BULK, class Off>
+__global__ void __launch_bounds__(32 * WR * WC, 16 / (WR * WC)) scan_backward_kernel(const __grid_constant__ ScanArgs A, const __grid_constant__ TileMaps maps) {
     constexpr int R = 8, GC = kChunkRows / R;              // 8 scale bytes are one load; groups of a chunk
+    static_assert(!BULK || (LX == 32 && WR == 8 && WC == 1), "the tiles and pieces of the tensor maps");
     using Pl = Place<V, LX, WR, WC, R>;
     using W = Raw<T, V>;
     using Q = std::conditional_t<V == 2, uint16_t, uint8_t>;
@@ -394,11 +494,24 @@ __global__ void __launch_bounds__(32 * WR * WC, 16 / (WR * WC)) scan_backward_ke
     static_assert(NG == 1 || TILE % kChunkRows == 0, "a tile holds whole chunks, or is the only one");
     __shared__ Exchange<V, LX, WR, WC, R> ex;
     __shared__ Cols<V> aggH[2][NG > 1 ? NG : 1][NG > 1 ? WC * LX : 1];
+    constexpr int ROW = 32 * V * S, QROW = SAVED8 ? 32 * V : ROW, ST = BACKWARD_STAGES;      // bytes of a row of dh, of gate and input
+    extern __shared__ __align__(128) unsigned char dynamic[];
+    using Here = BackwardTiles<T, V, SAVED8>;
+    [[maybe_unused]] Here& tiles = *reinterpret_cast<Here*>(on_128(dynamic));
+    auto* const sent = reinterpret_cast<Maps<V>*>(BULK ? on_128(dynamic) + sizeof(Here) : dynamic);
     Pl at(A);
     const int q = at.q, c = at.c, lane = at.col / V;
     const bool cv = at.cv;
     const int K = NG > 1 ? A.blocks : 1;
     ex.init(K);
+    if constexpr (BULK) {
+        if (threadIdx.x == 0) {
+#pragma unroll
+            for (int i = 0; i < ST; ++i) barrier_init(&tiles.arrived[i]);
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        }
+        __syncthreads();
+    }
     bool lost = false;
     const float none = S == 4 ? 0.0f : least_decay();
     dep_wait();
@@ -433,12 +546,18 @@ __global__ void __launch_bounds__(32 * WR * WC, 16 / (WR * WC)) scan_backward_ke
         constexpr bool FULL = decltype(full)::value;
         const int t = r0 + q * R, n = cv ? len - t : 0;
         if constexpr (SAVED8) {
-            const int64_t o = ((int64_t)at.b * A.rows + r0) * A.cols + at.first;
             if (FULL || n > 0) {
                 const int64_t os = ((int64_t)at.b * A.nblk + c / kBlock8) * A.rows_padded + t;
                 sg = *reinterpret_cast<const uint2*>(A.gs + os);
                 sx = *reinterpret_cast<const uint2*>(A.xs + os);
             }
+        }
+        const float* ps = A.states + ((int64_t)at.b * A.nchunk + t / kChunkRows) * A.cols + c;
+#pragma unroll
+        for (int v = 0; v < V; ++v) st.v[v] = FULL || n > 0 ? ps[v] : 0.0f;
+        if constexpr (BULK) return;
+        if constexpr (SAVED8) {
+            const int64_t o = ((int64_t)at.b * A.rows + r0) * A.cols + at.first;
 #pragma unroll
             for (int i = 0; i < R; ++i) {
                 qg[i] = FULL || i < n ? *reinterpret_cast<const Q*>(A.gq + (o + (int64_t)i * A.cols) + oq) : Q(0x8080);
@@ -455,15 +574,41 @@ __global__ void __launch_bounds__(32 * WR * WC, 16 / (WR * WC)) scan_backward_ke
         const char* d = bd + r0 * A.dh.row;
 #pragma unroll
         for (int i = 0; i < R; ++i) rd[i] = (FULL || i < n) && bd ? load_at<W>(d + i * A.dh.row + od) : W(0);
-        const float* ps = A.states + ((int64_t)at.b * A.nchunk + t / kChunkRows) * A.cols + c;
-#pragma unroll
-        for (int v = 0; v < V; ++v) st.v[v] = FULL || n > 0 ? ps[v] : 0.0f;
     };
     auto fetch = [&](int r0) {
         if (at.all && r0 + TILE <= len) fetch_rows(Yes{}, r0); else fetch_rows(No{}, r0);
     };
+    [[maybe_unused]] auto order = [&](int k) {             // one thread: the tile of the k-th step
+        uint64_t* bar = &tiles.arrived[k % ST];
+        unsigned char* to = tiles.in[k % ST];
+        const int row = ((steps - 1 - k) * K + at.rank) * TILE;
+        barrier_expect(bar, TILE * (2 * QROW + (bd ? ROW : 0)));
+        tile_load(to, maps.in[0], at.first, row, at.b, bar);
+        tile_load(to + TILE * QROW, maps.in[1], at.first, row, at.b, bar);
+        if (bd) tile_load(to + 2 * TILE * QROW, maps.in[2], at.first, row, at.b, bar);
+    };
+    [[maybe_unused]] auto take = [&](int k) {              // this thread's part of it
+        lost = !barrier_wait(&tiles.arrived[k % ST], (k / ST) & 1) || lost;
+        const unsigned char *from = tiles.in[k % ST] + q * R * QROW + at.col * (QROW / (32 * V)), *fd = tiles.in[k % ST] + 2 * TILE * QROW + q * R * ROW + at.col * S;
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            if constexpr (SAVED8) {
+                qg[i] = *reinterpret_cast<const Q*>(from + i * QROW);
+                qx[i] = *reinterpret_cast<const Q*>(from + TILE * QROW + i * QROW);
+            } else {
+                rg[i] = *reinterpret_cast<const W*>(from + i * QROW);
+                rx[i] = *reinterpret_cast<const W*>(from + TILE * QROW + i * QROW);
+            }
+            rd[i] = bd ? *reinterpret_cast<const W*>(fd + i * ROW) : W(0);
+        }
+    };
+    if constexpr (BULK) {
+        if (threadIdx.x == 0)
+            for (int k = 0; k < ST && k < steps; ++k) order(k);
+    }
     if (steps > 0) fetch(row0);
     if (K > 1) { cluster_arrive(); cluster_wait(); }
+    [[maybe_unused]] unsigned char* const mine_out = BULK ? tiles.out[threadIdx.x >> 5] + at.col * S : nullptr;
 
     Cols<V> a[R], w[R], x[R], d[R], P, H, M;
     auto prepare = [&](auto full, int n) {
@@ -480,21 +625,29 @@ __global__ void __launch_bounds__(32 * WR * WC, 16 / (WR * WC)) scan_backward_ke
                 zero_x |= any_zero_byte(wx);
             }
             if (!A.int8) zero_x = 0;
+#pragma unroll
+            for (int i = 0; i < R; ++i) w[i] = values_int8<V>(qg[i], scale_of(((i < 4 ? sg.x : sg.y) >> (8 * (i % 4))) & 255));
+            if (A.int8) {
+#pragma unroll
+                for (int i = 0; i < R; ++i) x[i] = values_int8<V>(qx[i], scale_of(((i < 4 ? sx.x : sx.y) >> (8 * (i % 4))) & 255));
+            } else {
+#pragma unroll
+                for (int i = 0; i < R; ++i) x[i] = values_e4m3<V>(qx[i], scale_of(((i < 4 ? sx.x : sx.y) >> (8 * (i % 4))) & 255));
+            }
+            if (zero_g | zero_x) {                         // rare: some value of this thread was not finite
+#pragma unroll
+                for (int i = 0; i < R; ++i)
+#pragma unroll
+                    for (int v = 0; v < V; ++v) {
+                        if (((qg[i] >> (8 * v)) & 255) == 0) w[i].v[v] = __uint_as_float(0x7fffffffu);
+                        if (A.int8 && ((qx[i] >> (8 * v)) & 255) == 0) x[i].v[v] = __uint_as_float(0x7fffffffu);
+                    }
+            }
         }
 #pragma unroll
         for (int i = 0; i < R; ++i) {
             if constexpr (SAVED8) {
-                const uint32_t bytes_g = i < 4 ? sg.x : sg.y, bytes_x = i < 4 ? sx.x : sx.y;
-                const float fg = scale_of((bytes_g >> (8 * (i % 4))) & 255), fx = scale_of((bytes_x >> (8 * (i % 4))) & 255);
-                Cols<V> g = values_int8<V>(qg[i], fg);
-                x[i] = A.int8 ? values_int8<V>(qx[i], fx) : values_e4m3<V>(qx[i], fx);
-                if (zero_g | zero_x) {                     // rare: some value of this thread was not finite
-#pragma unroll
-                    for (int v = 0; v < V; ++v) {
-                        if (((qg[i] >> (8 * v)) & 255) == 0) g.v[v] = __uint_as_float(0x7fffffffu);
-                        if (A.int8 && ((qx[i] >> (8 * v)) & 255) == 0) x[i].v[v] = __uint_as_float(0x7fffffffu);
-                    }
-                }
+                const Cols<V> g = w[i];
                 gates<S == 4>(g, a[i], w[i], none);
             } else {
                 gate_parts<T, V>(rg[i], a[i], w[i], none);
@@ -516,9 +669,22 @@ __global__ void __launch_bounds__(32 * WR * WC, 16 / (WR * WC)) scan_backward_ke
         for (int i = R - 1; i >= 0; --i) {
             const Cols<V> lam = add(d[i], mu), og_ = mul(lam, x[i]), ox_ = MIX ? mul(lam, w[i]) : lam;
             mu = mul(a[i], lam);
-            if (FULL || i < m) {
+            if constexpr (BULK) {
+                *reinterpret_cast<W*>(mine_out + i * ROW) = FULL || i < n ? join<T, V>(og_) : W(0);
+                *reinterpret_cast<W*>(mine_out + (R + i) * ROW) = FULL || i < n ? join<T, V>(ox_) : W(0);
+            } else if (FULL || i < m) {
                 store_at<W>(pdg + i * A.dg.row + odg, FULL || i < n ? join<T, V>(og_) : W(0));
                 store_at<W>(pdx + i * A.dx.row + odx, FULL || i < n ? join<T, V>(ox_) : W(0));
+            }
+        }
+        if constexpr (BULK) {
+            shared_to_bulk();
+            __syncwarp();
+            if ((threadIdx.x & 31) == 0 && row0 + q * R < A.rows) {
+                const unsigned char* from = tiles.out[threadIdx.x >> 5];
+                tile_store(maps.out[0], from, at.first, row0 + q * R, at.b);
+                tile_store(maps.out[1], from + R * ROW, at.first, row0 + q * R, at.b);
+                stores_commit();
             }
         }
     };
@@ -527,11 +693,18 @@ __global__ void __launch_bounds__(32 * WR * WC, 16 / (WR * WC)) scan_backward_ke
         const bool full = at.all && row0 + TILE <= len;
         const int t0 = row0 + q * R, n = cv ? len - t0 : 0, k = steps - 1 - s, buf = k & 1;
         Cols<V> hin = st;
+        if constexpr (BULK) {
+            take(k);
+            if ((threadIdx.x & 31) == 0) stores_read();    // the pieces of the step before
+            __syncwarp();
+        }
         if (full) prepare(Yes{}, n); else prepare(No{}, n);
-        if (s > 0) fetch(row0 - span);
+        if (s > 0) fetch(row0 - span);                     // (with bulk copies: states and scales)
 
         if constexpr (NG > 1) aggH[buf][q][lane] = H;
-        const Cols<V> mu = ex.template enter<true>(k, K, at.rank, q, lane, P, M, carry, lost, [&] {
+        const Cols<V> mu = ex.template enter<true>(sent, k, K, at.rank, q, lane, P, M, carry, lost, [&] {
+            if constexpr (BULK)
+                if (threadIdx.x == 0 && k + ST < steps) order(k + ST);          // the block has read this step's tile
             if constexpr (NG > 1)
                 for (int j = q - qc; j < q; ++j) hin = fma(ex.agg[buf][j][lane].p, hin, aggH[buf][j][lane]);
         });
@@ -551,50 +724,60 @@ __global__ void __launch_bounds__(32 * WR * WC, 16 / (WR * WC)) scan_backward_ke
 #pragma unroll
         for (int v = 0; v < V; ++v) A.end[(int64_t)at.b * A.cols + c + v] = carry.v[v];
     }
+    if (BULK && (threadIdx.x & 31) == 0) stores_done();
     if (K > 1) { cluster_arrive(); cluster_wait(); }
 }
 
 // ---- launches ----------------------------------------------------------------------------------------------------------------
-using Kernel = void (*)(ScanArgs);
+using Kernel = void (*)(ScanArgs, TileMaps);
 
 struct Shape {                   // of a launch
     Kernel kernel;
     int cols, tile, threads;     // columns and rows of a block
     bool split;                  // a column's rows may be shared by the blocks of a cluster
+    int tiles;                   // bytes of shared memory of the kernels that move their tiles by bulk copies, else 0
+    int piece;                   // rows that a warp of those stores
+    int sent;                    // bytes that a block of a cluster receives per block and step
+    int shared(int blocks) const { return (tiles ? tiles + 128 : 0) + (blocks > 1 ? 2 * blocks * sent : 0); }
 };
-template <int V, int LX, int WR, int WC, int R> Shape shape_of(Kernel k, bool split) {
+template <int V, int LX, int WR, int WC, int R> Shape shape_of(Kernel k, bool split, int tiles = 0) {
     using Pl = Place<V, LX, WR, WC, R>;
-    return Shape{k, Pl::COLS, Pl::TILE, Pl::THREADS, split};
+    return Shape{k, Pl::COLS, Pl::TILE, Pl::THREADS, split, tiles, R, WC * LX * (int)sizeof(Maps<V>)};
 }
 
-enum Layout { ONE_ROW, SHORT, TALL, NARROW, TALL_FAR };    // TALL_FAR: rows so far apart that offsets within a tile take 64 bits
+// TALL_FAR: rows so far apart that offsets within a tile take 64 bits; BULK: TALL with bulk copies of tiles
+enum Layout { ONE_ROW, SHORT, TALL, NARROW, TALL_FAR, BULK };
+using Near = uint32_t;
+using Far = int64_t;
 
 template <class T, int V, bool MIX> Shape forward_shape(Layout l, bool save8) {
-    using Near = uint32_t;
-    using Far = int64_t;
+    if constexpr (sizeof(T) * V == 4)
+        if (l == BULK)
+            return save8 ? shape_of<V, 32, 4, 1, 16>(scan_forward_kernel<T, V, 32, 4, 1, 16, true, MIX, true, Far>, true, sizeof(ForwardTiles<T, V, true>))
+                         : shape_of<V, 32, 4, 1, 16>(scan_forward_kernel<T, V, 32, 4, 1, 16, false, MIX, true, Far>, true, sizeof(ForwardTiles<T, V, false>));
     if (save8) switch (l) {
         case ONE_ROW:
-        case SHORT: return shape_of<V, 32, 1, 4, 16>(scan_forward_kernel<T, V, 32, 1, 4, 16, true, MIX, Near>, false);
-        case TALL_FAR: return shape_of<V, 32, 4, 1, 16>(scan_forward_kernel<T, V, 32, 4, 1, 16, true, MIX, Far>, true);
-        default: return shape_of<V, 32, 4, 1, 16>(scan_forward_kernel<T, V, 32, 4, 1, 16, true, MIX, Near>, true);
+        case SHORT: return shape_of<V, 32, 1, 4, 16>(scan_forward_kernel<T, V, 32, 1, 4, 16, true, MIX, false, Near>, false);
+        case TALL_FAR: return shape_of<V, 32, 4, 1, 16>(scan_forward_kernel<T, V, 32, 4, 1, 16, true, MIX, false, Far>, true);
+        default: return shape_of<V, 32, 4, 1, 16>(scan_forward_kernel<T, V, 32, 4, 1, 16, true, MIX, false, Near>, true);
     }
     switch (l) {
-        case ONE_ROW: return shape_of<V, 32, 1, 4, 1>(scan_forward_kernel<T, V, 32, 1, 4, 1, false, MIX, Near>, false);
-        case SHORT: return shape_of<V, 32, 1, 4, 16>(scan_forward_kernel<T, V, 32, 1, 4, 16, false, MIX, Near>, false);
-        case TALL: return shape_of<V, 32, 4, 1, 16>(scan_forward_kernel<T, V, 32, 4, 1, 16, false, MIX, Near>, true);
-        case TALL_FAR: return shape_of<V, 32, 4, 1, 16>(scan_forward_kernel<T, V, 32, 4, 1, 16, false, MIX, Far>, true);
-        default: return shape_of<V, 8, 4, 1, 16>(scan_forward_kernel<T, V, 8, 4, 1, 16, false, MIX, Near>, true);
+        case ONE_ROW: return shape_of<V, 32, 1, 4, 1>(scan_forward_kernel<T, V, 32, 1, 4, 1, false, MIX, false, Near>, false);
+        case SHORT: return shape_of<V, 32, 1, 4, 16>(scan_forward_kernel<T, V, 32, 1, 4, 16, false, MIX, false, Near>, false);
+        case NARROW: return shape_of<V, 8, 4, 1, 16>(scan_forward_kernel<T, V, 8, 4, 1, 16, false, MIX, false, Near>, true);
+        case TALL_FAR: return shape_of<V, 32, 4, 1, 16>(scan_forward_kernel<T, V, 32, 4, 1, 16, false, MIX, false, Far>, true);
+        default: return shape_of<V, 32, 4, 1, 16>(scan_forward_kernel<T, V, 32, 4, 1, 16, false, MIX, false, Near>, true);
     }
 }
 template <class T, int V, bool SAVED8, bool MIX> Shape backward_shape(Layout l) {
-    using Near = uint32_t;
-    using Far = int64_t;
+    if constexpr (sizeof(T) * V == 4)
+        if (l == BULK) return shape_of<V, 32, 8, 1, 8>(scan_backward_kernel<T, V, 32, 8, 1, SAVED8, MIX, true, Far>, true, sizeof(BackwardTiles<T, V, SAVED8>));
     switch (l) {
         case ONE_ROW:
-        case SHORT: return shape_of<V, 32, 1, 4, 8>(scan_backward_kernel<T, V, 32, 1, 4, SAVED8, MIX, Near>, false);
-        case TALL: return shape_of<V, 32, 8, 1, 8>(scan_backward_kernel<T, V, 32, 8, 1, SAVED8, MIX, Near>, true);
-        case TALL_FAR: return shape_of<V, 32, 8, 1, 8>(scan_backward_kernel<T, V, 32, 8, 1, SAVED8, MIX, Far>, true);
-        default: return shape_of<V, 8, 8, 1, 8>(scan_backward_kernel<T, V, 8, 8, 1, SAVED8, MIX, Near>, true);
+        case SHORT: return shape_of<V, 32, 1, 4, 8>(scan_backward_kernel<T, V, 32, 1, 4, SAVED8, MIX, false, Near>, false);
+        case NARROW: return shape_of<V, 8, 8, 1, 8>(scan_backward_kernel<T, V, 8, 8, 1, SAVED8, MIX, false, Near>, true);
+        case TALL_FAR: return shape_of<V, 32, 8, 1, 8>(scan_backward_kernel<T, V, 32, 8, 1, SAVED8, MIX, false, Far>, true);
+        default: return shape_of<V, 32, 8, 1, 8>(scan_backward_kernel<T, V, 32, 8, 1, SAVED8, MIX, false, Near>, true);
     }
 }
 template <class T, int V> Shape shape_for(bool mix, bool forward, bool save8, Layout l) {
@@ -617,14 +800,14 @@ constexpr int64_t MOST_GRID = 0x7fffffff;
 // Clusters of `blocks` blocks that the device holds at a time.
 int active_clusters(const Shape& f, int blocks) {
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(blocks); cfg.blockDim = dim3(f.threads);
+    cfg.gridDim = dim3(blocks); cfg.blockDim = dim3(f.threads); cfg.dynamicSmemBytes = f.shared(blocks);
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeClusterDimension;
     at[0].val.clusterDim.x = (unsigned)blocks; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
     cfg.attrs = at; cfg.numAttrs = 1;
     int n = 0;
     if (cudaFuncSetAttribute(f.kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess ||
-        cudaOccupancyMaxActiveClusters(&n, f.kernel, &cfg) != cudaSuccess) { (void)cudaGetLastError(); return 0; }
+        cudaFuncSetAttribute(f.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, f.shared(SCAN_MOST_BLOCKS)) != cudaSuccess || cudaOccupancyMaxActiveClusters(&n, f.kernel, &cfg) != cudaSuccess) { (void)cudaGetLastError(); return 0; }
     return n;
 }
 
@@ -661,6 +844,50 @@ int blocks_for(const Shape& f, int64_t n, int rows) {
     return best;
 }
 
+// ---- tensor maps -------------------------------------------------------------------------------------------------------------
+int element_bytes(int type) { return type == DN_F32 ? 4 : 2; }
+
+using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
+                                 CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiled encode_tiled() {                               // the driver's function, looked up once; NULL: the kernels without bulk copies serve
+    static const EncodeTiled f = [] {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess) {
+            (void)cudaGetLastError();
+            p = nullptr;
+        }
+        return reinterpret_cast<EncodeTiled>(p);
+    }();
+    return f;
+}
+// What a bulk copy asks of an array: 16-byte places and strides, none of them 0 (a row that all share), below 2^40 bytes.
+bool bulk_fits(const dn_scan& s, const RowsOf& r) {
+    if (!r.p) return true;
+    auto stride = [](int64_t n, int64_t b) { return n <= 1 || (b > 0 && b % 16 == 0 && b < ((int64_t)1 << 40)); };
+    return reinterpret_cast<uintptr_t>(r.p) % 16 == 0 && stride(s.rows, r.row) && stride(s.batch, r.batch);
+}
+bool tile_map(CUtensorMap* m, const dn_scan& s, const RowsOf& r, int type, int cols, int rows) {           // type: dn_type, or -1 for bytes
+    const CUtensorMapDataType t = type == DN_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : type == DN_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
+                                  : type == DN_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8;
+    const cuuint64_t dims[3] = {(cuuint64_t)s.cols, (cuuint64_t)s.rows, (cuuint64_t)s.batch};
+    const cuuint64_t strides[2] = {(cuuint64_t)r.row, (cuuint64_t)(s.batch > 1 ? r.batch : r.row)};       // (of one sample: any; there are more rows than one)
+    const cuuint32_t box[3] = {(cuuint32_t)cols, (cuuint32_t)rows, 1}, one[3] = {1, 1, 1};
+    return encode_tiled()(m, t, 3, r.p, dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+bool tile_maps(TileMaps* m, const dn_scan& s, const ScanArgs& A, bool forward, const Shape& f) {
+    const bool save8 = s.format != DN_SAVE_FULL;
+    const RowsOf gq{reinterpret_cast<char*>(A.gq), (int64_t)s.rows * s.cols, s.cols}, xq{reinterpret_cast<char*>(A.xq), (int64_t)s.rows * s.cols, s.cols};
+    if (forward)
+        return tile_map(&m->in[0], s, A.g, s.type, f.cols, f.tile) && tile_map(&m->in[1], s, A.x, s.type, f.cols, f.tile) &&
+               tile_map(&m->out[0], s, A.h, s.type, f.cols, f.piece) &&
+               (!save8 || (tile_map(&m->out[2], s, gq, -1, f.cols, f.piece) && tile_map(&m->out[3], s, xq, -1, f.cols, f.piece)));
+    return tile_map(&m->in[0], s, save8 ? gq : A.g, save8 ? -1 : s.type, f.cols, f.tile) &&
+           tile_map(&m->in[1], s, save8 ? xq : A.x, save8 ? -1 : s.type, f.cols, f.tile) && (!A.dh.p || tile_map(&m->in[2], s, A.dh, s.type, f.cols, f.tile)) &&
+           tile_map(&m->out[0], s, A.dg, s.type, f.cols, f.piece) && tile_map(&m->out[1], s, A.dx, s.type, f.cols, f.piece);
+}
+
 // Layout and blocks per cluster.  A sample's strip of columns is marched by one block where there are enough strips to fill the
 // device, else by a cluster along the rows; where even clusters of 16 leave SMs idle, strips of 8 lanes.
 dn_status launch(const dn_scan& s, bool pairs, bool forward, ScanArgs& A, cudaStream_t stream) {
@@ -669,12 +896,19 @@ dn_status launch(const dn_scan& s, bool pairs, bool forward, ScanArgs& A, cudaSt
     auto units = [&](const Shape& f) { return (((int64_t)s.cols + f.cols - 1) / f.cols) * s.batch; };
     Layout l = s.rows <= (forward ? 16 : 8) ? (s.rows <= 1 && !save8 ? ONE_ROW : SHORT) : TALL;
     Shape f = pick(s, pairs, forward, save8, l);
+    TileMaps maps{};
     if (l == TALL) {
         int64_t row = save8 ? s.cols : 0;                  // bytes between rows, at most
         for (const RowsOf& r : {A.g, A.x, A.h, A.dh, A.dg, A.dx}) row = r.row > row ? r.row : row;
         const bool far = (row + 1) * 64 + 4096 > (int64_t)UINT32_MAX, very = (row + 1) * 256 + 4096 > (int64_t)UINT32_MAX;
-        if (far) f = pick(s, pairs, forward, save8, TALL_FAR);
-        else if (!very && !(forward && save8) && units(f) * SCAN_MOST_BLOCKS < sms) f = pick(s, pairs, forward, save8, NARROW);
+        bool bulk = (s.type == DN_F32 || pairs) && (!save8 || s.cols % 16 == 0) && encode_tiled() != nullptr;
+        for (const RowsOf& r : {A.g, A.x, A.h, A.dh, A.dg, A.dx}) bulk = bulk && bulk_fits(s, r);
+        if (!far && !very && !(forward && save8) && units(f) * SCAN_MOST_BLOCKS < sms) f = pick(s, pairs, forward, save8, NARROW);
+        else {
+            const Shape g = pick(s, pairs, forward, save8, BULK);
+            if (bulk && tile_maps(&maps, s, A, forward, g)) f = g;
+            else if (far) f = pick(s, pairs, forward, save8, TALL_FAR);
+        }
     }
     int blocks = 1;
     const int64_t n = units(f);
@@ -683,20 +917,18 @@ dn_status launch(const dn_scan& s, bool pairs, bool forward, ScanArgs& A, cudaSt
     A.strips = (s.cols + f.cols - 1) / f.cols;
     A.blocks = blocks;
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)(n * blocks)); cfg.blockDim = dim3(f.threads); cfg.stream = stream;
+    cfg.gridDim = dim3((unsigned)(n * blocks)); cfg.blockDim = dim3(f.threads); cfg.stream = stream; cfg.dynamicSmemBytes = f.shared(blocks);
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     attr[1].id = cudaLaunchAttributeClusterDimension;
     attr[1].val.clusterDim.x = (unsigned)blocks; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr; cfg.numAttrs = blocks > 1 ? 2 : 1;
-    if (cudaLaunchKernelEx(&cfg, f.kernel, A) != cudaSuccess) { (void)cudaGetLastError(); return DN_ERR_CUDA; }
+    if (cudaLaunchKernelEx(&cfg, f.kernel, A, maps) != cudaSuccess) { (void)cudaGetLastError(); return DN_ERR_CUDA; }
     return DN_OK;
 }
 
 // ---- checks of arguments --------------------------------------------------------------------------------------------------------
-int element_bytes(int type) { return type == DN_F32 ? 4 : 2; }
-
 dn_status check(const dn_scan* s) {
     if (!s) return DN_ERR_NULL;
     if (s->batch < 1 || s->cols < 1 || s->rows < 0 || s->rows > (1 << 30) || s->cols > (1 << 30)) return DN_ERR_SIZE;
