@@ -245,13 +245,14 @@ template <class T, int V, bool SAVED8> using BackwardTiles =
     Tiles<BACKWARD_STAGES, 64 * 32 * V * (SAVED8 ? (int)sizeof(T) + 2 : 3 * (int)sizeof(T)), 8, 8 * 32 * V * 2 * (int)sizeof(T)>;
 
 template <class T, int V, int LX, int WR, int WC, int R, bool SAVE8, bool MIX, bool BULK, class Off>
-__global__ void __launch_bounds__(32 * WR * WC, SAVE8 ? 3 : 4) scan_forward_kernel(const __grid_constant__ ScanArgs A, const __grid_constant__ TileMaps maps) {
-    static_assert(!BULK || (LX == 32 && WR == 4 && WC == 1 && R == 16), "the tiles and pieces of the tensor maps");
-    static_assert(!SAVE8 || (LX == 32 && R == 16), "a row's 32 columns of a scale lie in one warp, 16 rows' scales in 16 lanes");
+__global__ void __launch_bounds__(32 * WR * WC, SAVE8 && !BULK ? 3 : 4) scan_forward_kernel(const __grid_constant__ ScanArgs A, const __grid_constant__ TileMaps maps) {
+    static_assert(!BULK || (WR == 4 && WC == 1 && R == 16), "the tiles and pieces of the tensor maps");
+    static_assert(!SAVE8 || (LX * V >= 32 && R == 16), "a row's 32 columns of a scale lie in one warp, 16 rows' scales in 16 lanes");
     using Pl = Place<V, LX, WR, WC, R>;
     using W = Raw<T, V>;
     constexpr int NG = Pl::NG, TILE = Pl::TILE, S = sizeof(T);
-    constexpr int ROW = 32 * V * S, ST = FORWARD_STAGES;   // bytes of a tile's row
+    constexpr int ROW = LX * V * S, ST = FORWARD_STAGES;   // bytes of a tile's row
+    [[maybe_unused]] constexpr int PIECE = 32 / LX * R;    // rows of a warp
     __shared__ Exchange<V, LX, WR, WC, R> ex;
     extern __shared__ __align__(128) unsigned char dynamic[];
     using Here = ForwardTiles<T, V, SAVE8>;
@@ -327,8 +328,9 @@ __global__ void __launch_bounds__(32 * WR * WC, SAVE8 ? 3 : 4) scan_forward_kern
             for (int s = 0; s < ST && s < steps; ++s) order(s);
     } else if (steps > 0) fetch(row0);
     if (K > 1) { cluster_arrive(); cluster_wait(); }       // every block of the cluster runs before one writes to another
-    [[maybe_unused]] unsigned char* const mine_out = BULK ? tiles.out[threadIdx.x >> 5] + at.col * S : nullptr;
-    [[maybe_unused]] unsigned char* const mine_codes = BULK ? tiles.out[threadIdx.x >> 5] + R * ROW + at.col : nullptr;
+    [[maybe_unused]] unsigned char* const mine_out = BULK ? tiles.out[threadIdx.x >> 5] + (threadIdx.x & 31) / LX * R * ROW + at.col * S : nullptr;
+    [[maybe_unused]] unsigned char* const mine_codes =
+        BULK ? tiles.out[threadIdx.x >> 5] + PIECE * ROW + (threadIdx.x & 31) / LX * R * LX * V + at.col : nullptr;
 
     // Codes and scales of this warp's 16 rows.  The largest magnitudes of the 16 rows are found together: at every stage of a butterfly a lane
     // hands half of its rows to the other and keeps the other's share of the rest, 15 exchanges of gate and input at once in place of 64
@@ -349,7 +351,7 @@ __global__ void __launch_bounds__(32 * WR * WC, SAVE8 ? 3 : 4) scan_forward_kern
             }
         if (V == 1) m[0] = __vmaxu2(m[0], __shfl_xor_sync(~0u, m[0], 16));
         const int eg = magnitude_exponent<T>(m[0] & 0xffffu), exx = magnitude_exponent<T>(m[0] >> 16);
-        const int block = at.first / kBlock8 + (threadIdx.x >> 5) / WR * V + (V == 2 ? lane >> 4 : 0);
+        const int block = (at.first + (threadIdx.x >> 5) / WR * LX * V) / kBlock8 + (LX * V == 64 ? lane >> 4 : 0);
         uint8_t *const gs = A.gs + ((int64_t)at.b * A.nblk + block) * A.rows_padded + t0, *const xs = A.xs + ((int64_t)at.b * A.nblk + block) * A.rows_padded + t0;
         const bool mine = block < A.nblk && t0 < A.rows_padded;
         uint8_t *const gq = A.gq + (((int64_t)at.b * A.rows + row0) * A.cols + at.first), *const xq = A.xq + (((int64_t)at.b * A.rows + row0) * A.cols + at.first);
@@ -357,8 +359,8 @@ __global__ void __launch_bounds__(32 * WR * WC, SAVE8 ? 3 : 4) scan_forward_kern
         auto put = [&](int i, uint32_t kg, uint32_t kx) {
             using Q = std::conditional_t<V == 2, uint16_t, uint8_t>;
             if constexpr (BULK) {
-                *reinterpret_cast<Q*>(mine_codes + i * 32 * V) = (Q)kg;
-                *reinterpret_cast<Q*>(mine_codes + (R + i) * 32 * V) = (Q)kx;
+                *reinterpret_cast<Q*>(mine_codes + i * LX * V) = (Q)kg;
+                *reinterpret_cast<Q*>(mine_codes + (PIECE + i) * LX * V) = (Q)kx;
             } else if (FULL || i < n) {
                 *reinterpret_cast<Q*>(gq + (int64_t)i * A.cols + oq) = (Q)kg;
                 *reinterpret_cast<Q*>(xq + (int64_t)i * A.cols + oq) = (Q)kx;
@@ -450,8 +452,8 @@ __global__ void __launch_bounds__(32 * WR * WC, SAVE8 ? 3 : 4) scan_forward_kern
                 const unsigned char* from = tiles.out[threadIdx.x >> 5];
                 tile_store(maps.out[0], from, at.first, t0, at.b);
                 if (SAVE8) {
-                    tile_store(maps.out[2], from + R * ROW, at.first, t0, at.b);
-                    tile_store(maps.out[3], from + R * ROW + R * 32 * V, at.first, t0, at.b);
+                    tile_store(maps.out[2], from + PIECE * ROW, at.first, t0, at.b);
+                    tile_store(maps.out[3], from + PIECE * ROW + PIECE * LX * V, at.first, t0, at.b);
                 }
                 stores_commit();
             }
@@ -654,7 +656,7 @@ __global__ void __launch_bounds__(32 * WR * WC, 16 / (WR * WC)) scan_backward_ke
                 x[i] = expand<T, V>(rx[i]);
             }
             d[i] = expand<T, V>(rd[i]);
-            if (!FULL && i >= n) { a[i] = all_of<V>(1.0f); w[i] = x[i] = all_of<V>(0.0f); }
+            if (!FULL && i >= n) { a[i] = all_of<V>(1.0f); w[i] = x[i] = d[i] = all_of<V>(0.0f); }
             const Cols<V> in = MIX ? mul(w[i], x[i]) : x[i];
             P = i ? mul(P, a[i]) : a[i];
             H = i ? fma(a[i], H, in) : in;
@@ -738,15 +740,17 @@ struct Shape {                   // of a launch
     int tiles;                   // bytes of shared memory of the kernels that move their tiles by bulk copies, else 0
     int piece;                   // rows that a warp of those stores
     int sent;                    // bytes that a block of a cluster receives per block and step
+    double latency;              // us of a step of a block that has its SM to itself
     int shared(int blocks) const { return (tiles ? tiles + 128 : 0) + (blocks > 1 ? 2 * blocks * sent : 0); }
 };
 template <int V, int LX, int WR, int WC, int R> Shape shape_of(Kernel k, bool split, int tiles = 0) {
     using Pl = Place<V, LX, WR, WC, R>;
-    return Shape{k, Pl::COLS, Pl::TILE, Pl::THREADS, split, tiles, R, WC * LX * (int)sizeof(Maps<V>)};
+    return Shape{k, Pl::COLS, Pl::TILE, Pl::THREADS, split, tiles, 32 / LX * R, WC * LX * (int)sizeof(Maps<V>), (R == 8 ? 1.1 : 0.8) + 0.15 * (32 / LX - 1)};
 }
 
-// TALL_FAR: rows so far apart that offsets within a tile take 64 bits; BULK: TALL with bulk copies of tiles
-enum Layout { ONE_ROW, SHORT, TALL, NARROW, TALL_FAR, BULK };
+// TALL_FAR: rows so far apart that offsets within a tile take 64 bits; BULK: TALL with bulk copies of tiles; BULK_HALF: strips of half the
+// columns and tiles of twice the rows (forward)
+enum Layout { ONE_ROW, SHORT, TALL, NARROW, TALL_FAR, BULK, BULK_HALF };
 using Near = uint32_t;
 using Far = int64_t;
 
@@ -755,6 +759,12 @@ template <class T, int V, bool MIX> Shape forward_shape(Layout l, bool save8) {
         if (l == BULK)
             return save8 ? shape_of<V, 32, 4, 1, 16>(scan_forward_kernel<T, V, 32, 4, 1, 16, true, MIX, true, Far>, true, sizeof(ForwardTiles<T, V, true>))
                          : shape_of<V, 32, 4, 1, 16>(scan_forward_kernel<T, V, 32, 4, 1, 16, false, MIX, true, Far>, true, sizeof(ForwardTiles<T, V, false>));
+    if constexpr (sizeof(T) * V == 4)
+        if (l == BULK_HALF && !save8)
+            return shape_of<V, 16, 4, 1, 16>(scan_forward_kernel<T, V, 16, 4, 1, 16, false, MIX, true, Far>, true, sizeof(ForwardTiles<T, V, false>));
+    if constexpr (V == 2)
+        if (l == BULK_HALF && save8)
+            return shape_of<V, 16, 4, 1, 16>(scan_forward_kernel<T, V, 16, 4, 1, 16, true, MIX, true, Far>, true, sizeof(ForwardTiles<T, V, true>));
     if (save8) switch (l) {
         case ONE_ROW:
         case SHORT: return shape_of<V, 32, 1, 4, 16>(scan_forward_kernel<T, V, 32, 1, 4, 16, true, MIX, false, Near>, false);
@@ -771,7 +781,7 @@ template <class T, int V, bool MIX> Shape forward_shape(Layout l, bool save8) {
 }
 template <class T, int V, bool SAVED8, bool MIX> Shape backward_shape(Layout l) {
     if constexpr (sizeof(T) * V == 4)
-        if (l == BULK) return shape_of<V, 32, 8, 1, 8>(scan_backward_kernel<T, V, 32, 8, 1, SAVED8, MIX, true, Far>, true, sizeof(BackwardTiles<T, V, SAVED8>));
+        if (l == BULK || l == BULK_HALF) return shape_of<V, 32, 8, 1, 8>(scan_backward_kernel<T, V, 32, 8, 1, SAVED8, MIX, true, Far>, true, sizeof(BackwardTiles<T, V, SAVED8>));
     switch (l) {
         case ONE_ROW:
         case SHORT: return shape_of<V, 32, 1, 4, 8>(scan_backward_kernel<T, V, 32, 1, 4, SAVED8, MIX, false, Near>, false);
@@ -811,23 +821,26 @@ int active_clusters(const Shape& f, int blocks) {
     return n;
 }
 
-// Blocks per cluster for n strips of columns, by an estimate of the time.  A step takes one latency (of loads, arithmetic and exchange),
-// and with all slots of an SM taken about two: measured, 1.2 to 1.4 us for one block per SM, 1.9 for two and 2.1 for 3.4 of 4 (64 rows
-// of 64 columns in 16 bits).  Two steps' time is added per wave for its start, 3 % per block that the others wait for.  32 strips of
-// 65536 rows: 1260 us with a block each, 364 with 4, 243 with 8; 16 take 272, since only 31 such clusters fit the device at a time.
-int blocks_for(const Shape& f, int64_t n, int rows) {
-    struct Known { Kernel kernel; int dev, rows, blocks; int64_t n; };
+// Blocks per cluster for n strips of columns and the time that they are estimated to take.
+//
+// A step takes a latency (loads, arithmetic, exchange: f.latency us), 0.2 us more where blocks wait for one another, and more the more blocks
+// share an SM, 1.4 us with all its slots taken; a wave takes 3 us to start and end.  Measured on 32 strips of 65536 rows of 64 columns in 16
+// bits, us per step (64 rows a block): a block each 0.88, clusters of 2 1.16, of 4 1.19, of 8 1.57 (201 us for all); of 16 1.93, but only 27 such
+// fit the device at a time (247 us).  As 64 strips of 32 columns, 128 rows a block: 1.03, 1.34, 1.65, clusters of 8 2.6 (168 us).
+struct Plan { int blocks; double time; };
+Plan plan_for(const Shape& f, int64_t n, int rows) {
+    struct Known { Kernel kernel; int dev, rows; int64_t n; Plan plan; };
     constexpr int KEPT = 16;
     thread_local Known known[KEPT] = {};                   // the last few answers: a function of the arguments and the device
     thread_local int next = 0;
     int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess) { (void)cudaGetLastError(); return 1; }
+    if (cudaGetDevice(&dev) != cudaSuccess) { (void)cudaGetLastError(); return Plan{1, 0.0}; }
     for (const Known& k : known)
-        if (k.kernel == f.kernel && k.dev == dev && k.rows == rows && k.n == n) return k.blocks;
+        if (k.kernel == f.kernel && k.dev == dev && k.rows == rows && k.n == n) return k.plan;
     const double sms = sm_count();
     const int64_t most = ((int64_t)rows + f.tile - 1) / f.tile;
-    int best = 1;
-    double least = 0.0, slots = 0.0;
+    Plan best{1, 1e30};
+    double slots = 1.0;
     for (int k = 1; k <= SCAN_MOST_BLOCKS && k <= most; ++k) {
         const int64_t active = active_clusters(f, k);
         if (active < 1) continue;
@@ -835,11 +848,11 @@ int blocks_for(const Shape& f, int64_t n, int rows) {
         const double waves = n < 3 * active ? (double)((n + active - 1) / active) : (double)n / active;
         const double steps = (double)((rows + (int64_t)k * f.tile - 1) / ((int64_t)k * f.tile));
         const double taken = (double)(n < active ? n : active) * k / sms;
-        const double t = waves * (steps + 2.0) * (1.0 + taken / slots) * (1.0 + 0.03 * (k - 1));
-        if (k == 1 || t < least) { least = t; best = k; }
+        const double t = waves * (steps * (f.latency + (k > 1 ? 0.2 + 0.01 * k : 0.0) + 1.4 * taken / slots) + 3.0);
+        if (t < best.time) best = Plan{k, t};
         if (waves > 4.0) break;                            // strips enough to fill the device several times
     }
-    known[next] = Known{f.kernel, dev, rows, best, n};
+    known[next] = Known{f.kernel, dev, rows, n, best};
     next = (next + 1) % KEPT;
     return best;
 }
@@ -906,13 +919,16 @@ dn_status launch(const dn_scan& s, bool pairs, bool forward, ScanArgs& A, cudaSt
         if (!far && !very && !(forward && save8) && units(f) * SCAN_MOST_BLOCKS < sms) f = pick(s, pairs, forward, save8, NARROW);
         else {
             const Shape g = pick(s, pairs, forward, save8, BULK);
-            if (bulk && tile_maps(&maps, s, A, forward, g)) f = g;
-            else if (far) f = pick(s, pairs, forward, save8, TALL_FAR);
+            if (bulk && tile_maps(&maps, s, A, forward, g)) {
+                f = g;
+                const Shape h = pick(s, pairs, forward, save8, BULK_HALF);
+                if (h.cols < g.cols && plan_for(h, units(h), s.rows).time < plan_for(g, units(g), s.rows).time && tile_maps(&maps, s, A, forward, h)) f = h;
+            } else if (far) f = pick(s, pairs, forward, save8, TALL_FAR);
         }
     }
     int blocks = 1;
     const int64_t n = units(f);
-    if (f.split) blocks = blocks_for(f, n, s.rows);
+    if (f.split) blocks = plan_for(f, n, s.rows).blocks;
     if (n * blocks > MOST_GRID) return DN_ERR_SIZE;
     A.strips = (s.cols + f.cols - 1) / f.cols;
     A.blocks = blocks;
