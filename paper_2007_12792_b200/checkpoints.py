@@ -48,14 +48,15 @@ class saved_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
         loss.backward()
 
     keep: tensors that stay as they are, views of them too (weights, which the gradient of the input multiplies with); so do
-    tensors of less than ``min_numel`` elements.  A gradient is then that of the ops at the values which 8 bits hold."""
+    tensors of less than ``min_numel`` elements.  A gradient is then that of the ops at the values which 8 bits hold.  A tensor that
+    several ops save is kept once for each of them."""
 
     def __init__(self, format: str = "int8", keep: Iterable[torch.Tensor] = (), min_numel: int = 4096):
         B._format(format)
         keep = tuple(keep)                                     # held: an address stands for its tensor only while that lives
 
         def put(t):
-            if not t.is_cuda or t.dtype not in TYPES or t.numel() < min_numel:
+            if not t.is_cuda or t.layout != torch.strided or t.dtype not in TYPES or t.numel() < min_numel:
                 return t
             place = t.untyped_storage().data_ptr()
             if any(k.is_cuda and k.untyped_storage().data_ptr() == place for k in keep):

@@ -196,7 +196,8 @@ PyObject* burgers_loss(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
 struct Device {
     c10::optional<c10::Device> one;
     void see(const at::Tensor& t, const char* name) {
-        TORCH_CHECK_VALUE(t.is_cuda(), name, ": expected a CUDA tensor (there is no CPU path)");
+        TORCH_CHECK_VALUE(t.is_cuda() && t.layout() == at::kStrided, name, ": expected a dense CUDA tensor (there is no CPU path)");
+        TORCH_CHECK_VALUE(!t.is_neg(), name, ": a negated view of other numbers; pass its resolve_neg()");
         if (!one) one = t.device();
         TORCH_CHECK_VALUE(*one == t.device(), name, ": on ", t.device(), ", the tensors ahead of it on ", *one);
     }
@@ -341,7 +342,11 @@ PyObject* scan_backward(PyObject*, PyObject* const* a, Py_ssize_t nargs) {     /
 }
 
 at::Tensor new_bytes(size_t n, const at::Tensor& like) { return at::empty({(int64_t)(n ? n : 1)}, like.options().dtype(at::kByte)); }
-at::Tensor with_adjacent_columns(const at::Tensor& t) { return !t.defined() || (t.dim() == 3 && (t.numel() == 0 || adjacent(t))) ? t : t.contiguous(); }
+at::Tensor with_adjacent_columns(const at::Tensor& u) {
+    const at::Tensor t = u.defined() ? u.resolve_neg() : u;
+    return !t.defined() || (t.dim() == 3 && (t.numel() == 0 || adjacent(t))) ? t : t.contiguous();
+}
+at::Tensor dense(const at::Tensor& t) { return t.defined() ? t.resolve_neg().contiguous() : t; }
 
 dn_scan scan_like(const at::Tensor& g, bool mix, int64_t format) {
     TORCH_CHECK_VALUE(g.dim() == 3, "gate: expected shape [batch, rows, cols], found ", g.sizes());
@@ -374,7 +379,7 @@ struct ScanFn : torch::autograd::Function<ScanFn> {
     static torch::autograd::variable_list forward(torch::autograd::AutogradContext* ctx, const at::Tensor& g_in, const at::Tensor& x_in, c10::optional<at::Tensor> h0_in,
                                                   c10::optional<at::Tensor> lengths_in, bool mix, int64_t format, int64_t status) {
         const at::Tensor none, g = with_adjacent_columns(g_in), x = with_adjacent_columns(x_in);
-        const at::Tensor h0 = h0_in ? h0_in->contiguous() : none, lengths = lengths_in ? *lengths_in : none;
+        const at::Tensor h0 = h0_in ? dense(*h0_in) : none, lengths = lengths_in ? *lengths_in : none;
         at::Tensor checkpoint;
         auto out = run(g, x, h0, lengths, mix, format, true, &checkpoint, reinterpret_cast<dn_status*>(status));
         // uint8: what packs the saved tensors of a step into 8 bits leaves the states in 32
@@ -402,7 +407,7 @@ struct ScanFn : torch::autograd::Function<ScanFn> {
         s.flags = ctx->saved_data["mix"].toBool() ? DN_SCAN_MIX : 0u;
         s.format = (int32_t)ctx->saved_data["format"].toInt();
         const bool full = s.format == DN_SAVE_FULL;
-        const at::Tensor &ck = saved[0], dh = with_adjacent_columns(grads[0]), dlast = grads[1].defined() ? grads[1].contiguous() : grads[1];
+        const at::Tensor &ck = saved[0], dh = with_adjacent_columns(grads[0]), dlast = dense(grads[1]);
         const at::Tensor g = full ? with_adjacent_columns(saved[1]) : none, x = full ? with_adjacent_columns(saved[2]) : none;
         Device d;
         bytes_checked(ck, "checkpoint", d);
@@ -443,7 +448,7 @@ PyObject* gated_scan(PyObject*, PyObject* const* a, Py_ssize_t nargs) {        /
             using Maybe = c10::optional<at::Tensor>;
             out = ScanFn::apply(g, x, h0.defined() ? Maybe(h0) : Maybe(), lengths.defined() ? Maybe(lengths) : Maybe(), mix != 0, format, reinterpret_cast<int64_t>(&st));
         }
-        else out = ScanFn::run(with_adjacent_columns(g), with_adjacent_columns(x), h0.defined() ? h0.contiguous() : h0, lengths, mix != 0, format, false, nullptr, &st);
+        else out = ScanFn::run(with_adjacent_columns(g), with_adjacent_columns(x), dense(h0), lengths, mix != 0, format, false, nullptr, &st);
     }
     if (st != DN_OK) return PyLong_FromLong((long)st);
     PyObject* r = PyTuple_New(2);
@@ -469,7 +474,7 @@ struct ActivationFn : torch::autograd::Function<ActivationFn> {
     }
     static at::Tensor forward(torch::autograd::AutogradContext* ctx, const at::Tensor& x, int64_t kind, int64_t format, int64_t status) {
         at::Tensor packed;
-        const at::Tensor y = run(x.contiguous(), kind, format, true, &packed, reinterpret_cast<dn_status*>(status));
+        const at::Tensor y = run(dense(x), kind, format, true, &packed, reinterpret_cast<dn_status*>(status));
         ctx->save_for_backward({packed});
         ctx->set_materialize_grads(false);
         ctx->saved_data["kind"] = kind;
@@ -480,7 +485,7 @@ struct ActivationFn : torch::autograd::Function<ActivationFn> {
         TORCH_CHECK(!at::GradMode::is_enabled(), "activation: the gradient is not differentiable again (create_graph)");
         const at::Tensor none;
         if (!grads[0].defined()) return {none, none, none, none};
-        const at::Tensor packed = ctx->get_saved_variables()[0], dy = grads[0].contiguous();
+        const at::Tensor packed = ctx->get_saved_variables()[0], dy = dense(grads[0]);
         Device d;
         bytes_checked(packed, "the saved input", d);
         d.see(dy, "dy");
@@ -505,7 +510,7 @@ PyObject* activation(PyObject*, PyObject* const* a, Py_ssize_t nargs) {        /
     {
         pybind11::gil_scoped_release no_gil;
         if (wants_grad({x})) y = ActivationFn::apply(x, kind, format, reinterpret_cast<int64_t>(&st));
-        else y = ActivationFn::run(x.contiguous(), kind, format, false, nullptr, &st);
+        else y = ActivationFn::run(dense(x), kind, format, false, nullptr, &st);
     }
     if (st != DN_OK) return PyLong_FromLong((long)st);
     return THPVariable_Wrap(y);
@@ -550,14 +555,14 @@ PyObject* packed(PyObject*, PyObject* const* a, Py_ssize_t nargs) {            /
     const at::Tensor& src = a_tensor(a[0], "src");
     const int32_t type = type_code(src.scalar_type(), "src"), format = small_integer(a[1], "format");
     Device d;
-    d.see(src, "src");
+    d.see(src.resolve_neg(), "src");
     c10::cuda::CUDAGuard guard(*d.one);
     at::Tensor out;
     dn_status st = DN_OK;
     {
         pybind11::gil_scoped_release no_gil;
         at::NoGradGuard no_grad;
-        const at::Tensor t = src.contiguous();
+        const at::Tensor t = dense(src);
         out = new_bytes(dn_packed_bytes(t.numel()), t);
         if (t.numel() > 0) st = dn_pack(t.numel(), type, t.data_ptr(), format, out.data_ptr(), c10::cuda::getCurrentCUDAStream(d.one->index()).stream());
     }

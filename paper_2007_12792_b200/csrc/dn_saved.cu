@@ -9,16 +9,20 @@
 namespace dn {
 namespace {
 
-constexpr int SAVED_THREADS = 256, UNIT = 8, UNITS = 4, PAIRS = UNIT / 2;
+constexpr int SAVED_THREADS = 256, UNIT = 8, UNITS = 2, PAIRS = UNIT / 2;
 
 __host__ __device__ constexpr int64_t scales_at(int64_t n) { return (n + 15) / 16 * 16; }
 
 using Pair = Cols<2>;
 template <class T> struct Unit { uint4 w[UNIT * sizeof(T) / 16]; };          // 8 values as they lie in memory
 
-template <class T> __device__ __forceinline__ Unit<T> load_unit(const T* p, int64_t i, int64_t n, bool wide) {
+template <class T> __device__ __forceinline__ Unit<T> load_unit(const T* p, int64_t i, int64_t n, int wide) {
     Unit<T> u;
-    if (wide && i + UNIT <= n) {
+    if (sizeof(T) == 4 && wide == 32 && i + UNIT <= n) {
+        constexpr int H = sizeof u / 16 - 1;               // (0, and not reached, for 16-bit types)
+        asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+            : "=r"(u.w[0].x), "=r"(u.w[0].y), "=r"(u.w[0].z), "=r"(u.w[0].w), "=r"(u.w[H].x), "=r"(u.w[H].y), "=r"(u.w[H].z), "=r"(u.w[H].w) : "l"(p + i) : "memory");
+    } else if (wide && i + UNIT <= n) {
 #pragma unroll
         for (int k = 0; k < (int)(UNIT * sizeof(T) / 16); ++k) u.w[k] = reinterpret_cast<const uint4*>(p + i)[k];
     } else {
@@ -35,15 +39,21 @@ template <class T> __device__ __forceinline__ void values_in(const Unit<T>& u, P
 #pragma unroll
     for (int j = 0; j < PAIRS; ++j) f[j] = Pair{{as_float(t[2 * j]), as_float(t[2 * j + 1])}};
 }
-template <class T> __device__ __forceinline__ void store_unit(T* p, int64_t i, int64_t n, bool wide, const Pair (&f)[PAIRS]) {
+template <class T> __device__ __forceinline__ void store_unit(T* p, int64_t i, int64_t n, int wide, const Pair (&f)[PAIRS]) {
     T t[UNIT];
 #pragma unroll
     for (int j = 0; j < UNIT; ++j) t[j] = rounded<T>(f[j / 2].v[j % 2]);
     if (wide && i + UNIT <= n) {
         Unit<T> u;
         memcpy(&u, t, sizeof u);
+        if (sizeof(T) == 4 && wide == 32) {
+            constexpr int H = sizeof u / 16 - 1;
+            asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p + i), "r"(u.w[0].x), "r"(u.w[0].y), "r"(u.w[0].z), "r"(u.w[0].w),
+                         "r"(u.w[H].x), "r"(u.w[H].y), "r"(u.w[H].z), "r"(u.w[H].w) : "memory");
+        } else {
 #pragma unroll
-        for (int k = 0; k < (int)(UNIT * sizeof(T) / 16); ++k) reinterpret_cast<uint4*>(p + i)[k] = u.w[k];
+            for (int k = 0; k < (int)(UNIT * sizeof(T) / 16); ++k) reinterpret_cast<uint4*>(p + i)[k] = u.w[k];
+        }
     } else {
 #pragma unroll
         for (int j = 0; j < UNIT; ++j)
@@ -198,7 +208,7 @@ template <int KIND, bool ACCURATE> __device__ __forceinline__ Pair slope(Pair x)
     }
 }
 
-template <class T> __global__ void __launch_bounds__(SAVED_THREADS) pack_kernel(int64_t n, const T* src, int int8, uint8_t* packed, bool wide) {
+template <class T> __global__ void __launch_bounds__(SAVED_THREADS) pack_kernel(int64_t n, const T* src, int int8, uint8_t* packed, int wide) {
     dep_wait();
     const int64_t first = ((int64_t)blockIdx.x * SAVED_THREADS * UNITS + threadIdx.x) * UNIT;
     Unit<T> w[UNITS];
@@ -211,7 +221,7 @@ template <class T> __global__ void __launch_bounds__(SAVED_THREADS) pack_kernel(
         store_codes(packed, first + (int64_t)u * SAVED_THREADS * UNIT, n, int8, w[u], f);
     }
 }
-template <class T> __global__ void __launch_bounds__(SAVED_THREADS) unpack_kernel(int64_t n, T* dst, int int8, const uint8_t* packed, bool wide) {
+template <class T> __global__ void __launch_bounds__(SAVED_THREADS) unpack_kernel(int64_t n, T* dst, int int8, const uint8_t* packed, int wide) {
     dep_wait();
     const int64_t first = ((int64_t)blockIdx.x * SAVED_THREADS * UNITS + threadIdx.x) * UNIT;
     Codes r[UNITS];
@@ -225,7 +235,7 @@ template <class T> __global__ void __launch_bounds__(SAVED_THREADS) unpack_kerne
     }
 }
 template <class T, int KIND>
-__global__ void __launch_bounds__(SAVED_THREADS) activation_forward_kernel(int64_t n, const T* x, T* y, int int8, uint8_t* packed, bool wide) {
+__global__ void __launch_bounds__(SAVED_THREADS) activation_forward_kernel(int64_t n, const T* x, T* y, int int8, uint8_t* packed, int wide) {
     dep_wait();
     const int64_t first = ((int64_t)blockIdx.x * SAVED_THREADS * UNITS + threadIdx.x) * UNIT;
     Unit<T> w[UNITS];
@@ -243,7 +253,7 @@ __global__ void __launch_bounds__(SAVED_THREADS) activation_forward_kernel(int64
     }
 }
 template <class T, int KIND>
-__global__ void __launch_bounds__(SAVED_THREADS) activation_backward_kernel(int64_t n, const uint8_t* packed, int int8, const T* dy, T* dx, bool wide) {
+__global__ void __launch_bounds__(SAVED_THREADS) activation_backward_kernel(int64_t n, const uint8_t* packed, int int8, const T* dy, T* dx, int wide) {
     dep_wait();
     const int64_t first = ((int64_t)blockIdx.x * SAVED_THREADS * UNITS + threadIdx.x) * UNIT;
     Unit<T> w[UNITS];
@@ -274,6 +284,11 @@ dn_status check(int64_t n, int type, int format) {
 size_t bytes_of(int64_t n, int type) { return (size_t)n * (type == DN_F32 ? 4 : 2); }
 bool off(const void* p, int type) { return reinterpret_cast<uintptr_t>(p) % (type == DN_F32 ? 4 : 2) != 0; }
 bool off16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 != 0; }
+// bytes of an access: 32 (32-bit types), 16, or element by element (0)
+int width(const void* a, const void* b) {
+    const uintptr_t both = reinterpret_cast<uintptr_t>(a) | reinterpret_cast<uintptr_t>(b);
+    return both % 32 == 0 ? 32 : both % 16 == 0 ? 16 : 0;
+}
 bool meet(const void* a, size_t na, const void* b, size_t nb) {
     const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
     return x < y + nb && y < x + na;
@@ -285,11 +300,11 @@ template <typename... KArgs, typename... Args> dn_status go(void (*kernel)(KArgs
     (void)cudaGetLastError();
     return DN_ERR_CUDA;
 }
-template <class T> dn_status activate(int64_t n, int kind, const void* x, void* y, int int8, void* packed, bool wide, void* stream) {
+template <class T> dn_status activate(int64_t n, int kind, const void* x, void* y, int int8, void* packed, int wide, void* stream) {
     auto k = kind == DN_SILU ? activation_forward_kernel<T, DN_SILU> : kind == DN_GELU ? activation_forward_kernel<T, DN_GELU> : activation_forward_kernel<T, DN_TANH>;
     return go(k, n, stream, n, static_cast<const T*>(x), static_cast<T*>(y), int8, static_cast<uint8_t*>(packed), wide);
 }
-template <class T> dn_status differentiate(int64_t n, int kind, const void* packed, int int8, const void* dy, void* dx, bool wide, void* stream) {
+template <class T> dn_status differentiate(int64_t n, int kind, const void* packed, int int8, const void* dy, void* dx, int wide, void* stream) {
     auto k = kind == DN_SILU ? activation_backward_kernel<T, DN_SILU> : kind == DN_GELU ? activation_backward_kernel<T, DN_GELU> : activation_backward_kernel<T, DN_TANH>;
     return go(k, n, stream, n, static_cast<const uint8_t*>(packed), int8, static_cast<const T*>(dy), static_cast<T*>(dx), wide);
 }
@@ -314,7 +329,7 @@ dn_status dn_pack(int64_t n, int32_t type, const void* src, int32_t format, void
     if (off(src, type) || off16(packed)) return DN_ERR_LAYOUT;
     if (meet(src, bytes_of(n, type), packed, dn_packed_bytes(n))) return DN_ERR_ALIAS;
     const int int8 = format == DN_INT8;
-    const bool wide = !off16(src);
+    const int wide = width(src, src);
     uint8_t* q = static_cast<uint8_t*>(packed);
     if (type == DN_F32) return go(pack_kernel<float>, n, stream, n, static_cast<const float*>(src), int8, q, wide);
     if (type == DN_BF16) return go(pack_kernel<__nv_bfloat16>, n, stream, n, static_cast<const __nv_bfloat16*>(src), int8, q, wide);
@@ -327,7 +342,7 @@ dn_status dn_unpack(int64_t n, int32_t type, const void* packed, int32_t format,
     if (off(dst, type) || off16(packed)) return DN_ERR_LAYOUT;
     if (meet(dst, bytes_of(n, type), packed, dn_packed_bytes(n))) return DN_ERR_ALIAS;
     const int int8 = format == DN_INT8;
-    const bool wide = !off16(dst);
+    const int wide = width(dst, dst);
     const uint8_t* q = static_cast<const uint8_t*>(packed);
     if (type == DN_F32) return go(unpack_kernel<float>, n, stream, n, static_cast<float*>(dst), int8, q, wide);
     if (type == DN_BF16) return go(unpack_kernel<__nv_bfloat16>, n, stream, n, static_cast<__nv_bfloat16*>(dst), int8, q, wide);
@@ -342,7 +357,7 @@ dn_status dn_activation_forward(int64_t n, int32_t type, int32_t kind, const voi
     const size_t b = bytes_of(n, type), k = packed ? dn_packed_bytes(n) : 0;
     if (meet(x, b, y, b) || meet(x, b, packed, k) || meet(y, b, packed, k)) return DN_ERR_ALIAS;
     const int int8 = format == DN_INT8;
-    const bool wide = !off16(x) && !off16(y);
+    const int wide = width(x, y);
     if (type == DN_F32) return activate<float>(n, kind, x, y, int8, packed, wide, stream);
     if (type == DN_BF16) return activate<__nv_bfloat16>(n, kind, x, y, int8, packed, wide, stream);
     return activate<__half>(n, kind, x, y, int8, packed, wide, stream);
@@ -356,7 +371,7 @@ dn_status dn_activation_backward(int64_t n, int32_t type, int32_t kind, const vo
     const size_t b = bytes_of(n, type), k = dn_packed_bytes(n);
     if ((dx != dy && meet(dx, b, dy, b)) || meet(dx, b, packed, k)) return DN_ERR_ALIAS;
     const int int8 = format == DN_INT8;
-    const bool wide = !off16(dy) && !off16(dx);
+    const int wide = width(dy, dx);
     if (type == DN_F32) return differentiate<float>(n, kind, packed, int8, dy, dx, wide, stream);
     if (type == DN_BF16) return differentiate<__nv_bfloat16>(n, kind, packed, int8, dy, dx, wide, stream);
     return differentiate<__half>(n, kind, packed, int8, dy, dx, wide, stream);

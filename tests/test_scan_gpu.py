@@ -322,6 +322,42 @@ def test_streams_graphs_and_repetition(fmt):
         assert torch.equal(u, v)
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("odd", [0, 1])
+def test_rows_far_apart(dtype, odd):
+    """Rows of one wide array, 64 MiB and more apart: offsets within a tile pass 32 bits.  odd: off the 16 bytes of a bulk copy."""
+    T, C, W = 70, 8, (1 << 26) // (4 if dtype == F32 else 2) + 64
+    wide = torch.empty(1, T, W, dtype=dtype, device="cuda")
+    part = lambda k: wide[:, :, 16 * k + odd * 2:16 * k + odd * 2 + C]
+    g, x, h0, _, dh, dh_last = random_case(1, T, C, dtype, 8)
+    for k, t in enumerate((g, x, dh)):
+        part(k).copy_(t)
+    for fmt in (None, "int8"):
+        p, h, h_last, ck = call_forward(part(0), part(1), h0, None, True, fmt, h=part(3))
+        dh0 = torch.empty_like(h0)
+        B.dn_scan_backward(p, part(0), part(1), ck, part(2), dh_last, part(4), part(5), dh0)
+        wh, _, _, eh, _, _ = S.forward(g, x, h0, None, True)
+        wg, wx, w0, eg, ex, e0 = S.backward(g, x, h0, None, True, dh, dh_last, fmt)
+        for got, want, err, d in ((part(3), wh, eh, dtype), (part(4), wg, eg, dtype), (part(5), wx, ex, dtype), (dh0, w0, e0, F32)):
+            S.check(got, want, err, d)
+
+
+def test_negated_views():
+    """Complex conjugates hand out views whose sign is only noted: the ops resolve them, the calls on buffers refuse them."""
+    g, x, h0, _, dh, _ = random_case(2, 20, 8, F32, 2)
+    neg = torch.complex(x, x).conj().imag
+    assert neg.is_neg()
+    h, _ = autograd.gated_scan(g, neg, h0)
+    want, _ = autograd.gated_scan(g, -x, h0)
+    assert torch.equal(h, want)
+    flat = torch._neg_view(x)
+    assert torch.equal(autograd.activation(flat), autograd.activation(-x))
+    from paper_2007_12792_b200 import checkpoints
+    assert torch.equal(checkpoints.pack(flat).unpack(), checkpoints.pack(-x).unpack())
+    with pytest.raises(ValueError, match="negated"):
+        B.dn_scan_forward(B.Scan(2, 20, 8), torch._neg_view(g), x, h0, torch.empty_like(g), None)
+
+
 def test_offsets_beyond_32_bits():
     """2.2e9 elements: the last rows, from short memories, against a recurrence over the last 200 rows alone (2^-100 is left of what
     was before them)."""
