@@ -283,7 +283,9 @@ const char* dn_kernel_name(const dn_problem* problem, const float* u, const floa
  *
  * Back-propagation (Algorithm 1) passes through the generator on its way from the loss to the weights, and the memory of its
  * intermediate tensors is what bounds the size of the fields ("DiffNets": about 64 GB at 512^2 with 64 samples).  These entry points
- * take fields in 32 or 16 bits; all arithmetic is in 32 bits, each result is rounded once. */
+ * take fields in 32 or 16 bits; all arithmetic is in 32 bits, each result is rounded once.  Results depend on no order of execution: no
+ * atomics.  Where the blocks of a thread-block cluster wait for one another or for a copy, the wait has a limit; should it ever run out,
+ * the results behind it are NaN. */
 typedef enum { DN_F32 = 0, DN_BF16 = 1, DN_F16 = 2 } dn_type;
 
 /* Values in 8 bits: blocks of 32 share a scale 2^e.  With A the largest finite magnitude of a block, 2^k <= A < 2^(k+1):
@@ -304,8 +306,8 @@ typedef struct {
  *   a_t = 1 / (1 + exp(-g_t)),   w_t = 1, or 1 - a_t with DN_SCAN_MIX
  *   h_t = a_t h_{t-1} + w_t x_t,   t = 0 .. n_b - 1,   h_{-1} = h0 (0 where h0 is NULL)
  *
- * n_b = rows, or lengths[b] (values outside 0 .. rows count as the nearer of the two).  Rows from n_b on are not read; h, dg and dx
- * are 0 there.  h_last[b] = h_{n_b - 1} (h0[b] if n_b = 0). */
+ * n_b = rows, or lengths[b] (values outside 0 .. rows count as the nearer of the two).  What stands in rows from n_b on, NaN included,
+ * plays no part; h, dg and dx are 0 there.  h_last[b] = h_{n_b - 1} (h0[b] if n_b = 0). */
 #define DN_SCAN_MIX 1u
 #define DN_SCAN_CHUNK 64         /* rows between two states that a checkpoint keeps in 32 bits */
 typedef struct {
@@ -335,7 +337,8 @@ dn_status dn_scan_forward(const dn_scan* scan, const dn_rows* g, const dn_rows* 
 dn_status dn_scan_backward(const dn_scan* scan, const dn_rows* g, const dn_rows* x, const void* checkpoint, size_t checkpoint_bytes,
                            const dn_rows* dh, const float* dh_last, const dn_rows* dg, const dn_rows* dx, float* dh0, void* stream);
 
-/* n values in 8 bits, blocks of 32 as they lie in memory: dn_packed_bytes(n) bytes, 16-byte aligned. */
+/* n values in 8 bits, blocks of 32 as they lie in memory: dn_packed_bytes(n) bytes, 16-byte aligned (the codes, padded to 16 bytes, then
+ * a byte per block for its scale; 0 if n is out of range).  src, dst and packed must not overlap. */
 size_t dn_packed_bytes(int64_t n);
 dn_status dn_pack(int64_t n, int32_t type, const void* src, int32_t format, void* packed, void* stream);
 dn_status dn_unpack(int64_t n, int32_t type, const void* packed, int32_t format, void* dst, void* stream);

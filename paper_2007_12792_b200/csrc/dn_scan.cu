@@ -660,9 +660,8 @@ __global__ void __launch_bounds__(32 * WR * WC, 16 / (WR * WC)) scan_backward_ke
             const Cols<V> in = MIX ? mul(w[i], x[i]) : x[i];
             P = i ? mul(P, a[i]) : a[i];
             H = i ? fma(a[i], H, in) : in;
+            M = i ? fma(d[i], P, M) : mul(d[i], P);        // what enters row i passes through a_i .. a_0
         }
-#pragma unroll
-        for (int i = R - 1; i >= 0; --i) M = mul(a[i], i < R - 1 ? add(d[i], M) : d[i]);
     };
     auto write = [&](auto full, int n, int m, Cols<V> mu) {
         constexpr bool FULL = decltype(full)::value;
