@@ -462,7 +462,11 @@ class Scan:
     lengths: Optional[torch.Tensor] = None     # [batch] int32 on the device
 
     def __post_init__(self):
-        self.format = _format(self.checkpoint, none=True)
+        _format(self.checkpoint, none=True)
+
+    @property
+    def format(self) -> int:
+        return _format(self.checkpoint, none=True)
 
     @property
     def shape(self):

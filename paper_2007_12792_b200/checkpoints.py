@@ -53,14 +53,15 @@ class saved_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
 
     def __init__(self, format: str = "int8", keep: Iterable[torch.Tensor] = (), min_numel: int = 4096):
         B._format(format)
-        keep = tuple(keep)                                     # held: an address stands for its tensor only while that lives
+        self._keep, self._places = tuple(keep), frozenset()    # held: an address stands for its tensor only while that lives
 
         def put(t):
             if not t.is_cuda or t.layout != torch.strided or t.dtype not in TYPES or t.numel() < min_numel:
                 return t
-            place = t.untyped_storage().data_ptr()
-            if any(k.is_cuda and k.untyped_storage().data_ptr() == place for k in keep):
-                return t
-            return pack(t, format)
+            return t if t.untyped_storage().data_ptr() in self._places else pack(t, format)
 
         super().__init__(put, lambda p: p.unpack() if isinstance(p, Packed) else p)
+
+    def __enter__(self):
+        self._places = frozenset(k.untyped_storage().data_ptr() for k in self._keep if k.is_cuda)
+        return super().__enter__()

@@ -279,7 +279,8 @@ __global__ void __launch_bounds__(SAVED_THREADS) activation_backward_kernel(int6
     }
 }
 
-constexpr int64_t MOST_VALUES = (int64_t)1 << 43;          // blocks of a launch stay below 2^31
+constexpr int64_t MOST_VALUES = (int64_t)1 << 42;          // blocks of a launch stay below 2^31
+static_assert(MOST_VALUES / (SAVED_THREADS * UNITS * UNIT) < 0x7fffffff, "");
 
 dn_status check(int64_t n, int type, int format) {
     if (n < 1 || n > MOST_VALUES) return DN_ERR_SIZE;

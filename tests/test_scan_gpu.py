@@ -236,6 +236,44 @@ def test_gradients_by_differences():
                 assert abs(float(got[k][place]) - want) <= float(e[place]) + 2.0 ** -24 * abs(want) + 1e-7, (mix, k, place)
 
 
+def test_no_rows_as_a_torch_op():
+    g = torch.empty(3, 0, 5, device="cuda", requires_grad=True)
+    x, h0 = torch.empty(3, 0, 5, device="cuda", requires_grad=True), torch.randn(3, 5, device="cuda", requires_grad=True)
+    for fmt in (None, "int8"):
+        h, last = autograd.gated_scan(g, x, h0, checkpoint=fmt)
+        assert h.shape == (3, 0, 5) and torch.equal(last, h0)
+        d = torch.randn(3, 5, device="cuda")
+        dg, dx, dh0 = torch.autograd.grad(last, (g, x, h0), d)
+        assert dg.shape == dx.shape == (3, 0, 5) and torch.equal(dh0, d)
+
+
+def test_the_first_call_of_a_process_may_be_captured():
+    """A child process whose first calls stand in a graph: what they ask the device for is no work on a stream."""
+    import subprocess
+    import sys
+    code = """
+import torch
+from paper_2007_12792_b200 import autograd, binding as B
+g, x, d = (torch.randn(2, 1200, 64, device="cuda", dtype=torch.bfloat16) for _ in range(3))
+p = B.Scan(2, 1200, 64, dtype=torch.bfloat16, mix=True, checkpoint="int8")
+h, dg, dx, last, ck = torch.empty_like(g), torch.empty_like(g), torch.empty_like(g), torch.empty(2, 64, device="cuda"), B.new_scan_checkpoint(p)
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    B.dn_scan_forward(p, g, x, None, h, last, ck)
+    B.dn_scan_backward(p, None, None, ck, d, None, dg, dx, None)
+graph.replay()
+torch.cuda.synchronize()
+out = [t.clone() for t in (h, last, dg, dx)]
+B.dn_scan_forward(p, g, x, None, h, last, ck)
+B.dn_scan_backward(p, None, None, ck, d, None, dg, dx, None)
+assert all(torch.equal(a, b) for a, b in zip(out, (h, last, dg, dx)))
+print("same")
+"""
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "same" in r.stdout, r.stderr[-2000:]
+
+
 def test_no_second_derivative():
     g, x, _, _, dh, _ = random_case(1, 20, 8, F32, 1)
     x.requires_grad_()
