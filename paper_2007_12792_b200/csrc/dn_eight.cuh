@@ -167,16 +167,9 @@ __device__ __forceinline__ unsigned code_e4m3(float v, float inverse) {
 }
 __device__ __forceinline__ unsigned code8(float v, float inverse, bool int8) { return int8 ? code_int8(v, inverse) : code_e4m3(v, inverse); }
 
-// an integer 0 .. 255 set into the last bits of 2^23 becomes a float without the conversion unit, which the exponentials need
-__device__ __forceinline__ float value_int8(unsigned code, float scale) {
-    const float v = (__uint_as_float(0x4b000000u | code) - 8388736.0f) * scale;
-    return code ? v : __uint_as_float(0x7fffffffu);
-}
 __device__ __forceinline__ float value_e4m3(unsigned code, float scale) {
     return __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)code, __NV_E4M3))) * scale;
 }
-__device__ __forceinline__ float value8(unsigned code, float scale, bool int8) { return int8 ? value_int8(code, scale) : value_e4m3(code, scale); }
-
 // Codes of V adjacent columns, first column in the lowest byte.  v / 2^e + 2^23 + 2^22 + 128 is rounded to an integer by the sum itself
 // (the quotient is exact, and inside a fused product and sum not even formed); the code then stands in the last bits.  The values are
 // finite.
@@ -195,7 +188,7 @@ __device__ __forceinline__ uint32_t codes_e4m3(const Cols<2>& v, float inverse) 
     const float2 h = make_float2(fminf(fmaxf(t.v[0], -240.0f), 240.0f), fminf(fmaxf(t.v[1], -240.0f), 240.0f));
     return (uint32_t)__nv_cvt_float2_to_fp8x2(h, __NV_SATFINITE, __NV_E4M3);
 }
-// ... and back.  A code 0, not a number, is read as -128 here: the caller looks for it (any_zero_byte).
+// ... and back: a code set into the last bits of 2^23 is a float without the conversion unit, which the exponentials need.  A code 0, not a number, is read as -128 here: the caller looks for it (any_zero_byte).
 template <int V> __device__ __forceinline__ Cols<V> values_int8(uint32_t codes, float scale) {
     Cols<V> f;
     f.v[0] = __uint_as_float(__byte_perm(codes, 0x4b000000u, 0x7440));
