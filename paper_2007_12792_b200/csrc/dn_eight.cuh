@@ -21,7 +21,7 @@
 namespace dn {
 
 constexpr int kBlock8 = 32;            // values that share a scale
-constexpr int kChunkRows = 64;         // rows between two states that a checkpoint of the scan keeps in 32 bits
+constexpr int kChunkRows = DN_SCAN_CHUNK;  // rows between two states that a checkpoint of the scan keeps in 32 bits
 
 // Where things live in a checkpoint of the scan (byte offsets, 256-byte aligned): codes [batch][rows][cols] of gate and input, their
 // scales [batch][blocks of 32 columns][rows, padded to a multiple of 64] (rows innermost: a thread that owns consecutive rows of a
