@@ -77,7 +77,7 @@ def gated_scan(gate: torch.Tensor, x: torch.Tensor, h0: Optional[torch.Tensor] =
                mix: bool = False, checkpoint: Optional[str] = None) -> Tuple[torch.Tensor, torch.Tensor]:
     """(h, h_last) of the recurrence h_t = a_t h_{t-1} + w_t x_t over the rows of fields [batch, rows, cols], a = sigmoid(gate),
     w = 1 or, with ``mix``, 1 - a; h0 and h_last: [batch, cols] float32; lengths: [batch] int32, rows behind them are 0.
-    gate and x: CUDA tensors of one type (float32, bfloat16, float16).  Differentiable once, with respect to gate, x and h0.
+    gate and x: CUDA tensors of one type (float32, bfloat16, float16).  Differentiable once, backward, with respect to gate, x and h0.
 
     checkpoint None keeps gate, x and the state ahead of every 64th row for the backward pass; "int8" or "e4m3" keeps gate and x
     in 8 bits instead (the gate as int8 in either), and the gradients are those at the values that 8 bits hold."""
@@ -89,7 +89,7 @@ def gated_scan(gate: torch.Tensor, x: torch.Tensor, h0: Optional[torch.Tensor] =
 
 def activation(x: torch.Tensor, kind: str = "silu", checkpoint: str = "int8") -> torch.Tensor:
     """"silu", "gelu" (its tanh form) or "tanh" of a CUDA tensor, which keeps its input for the backward pass in 8 bits ("int8" or
-    "e4m3"): the gradient is dy f'(x) at the values that 8 bits hold.  Differentiable once."""
+    "e4m3"): the gradient is dy f'(x) at the values that 8 bits hold.  Differentiable once, backward."""
     y = B.native().activation(x, B._kind(kind), B._format(checkpoint))
     if isinstance(y, int):
         raise B.DnError(y, "dn_activation_forward")

@@ -13,6 +13,7 @@
 #include <torch/csrc/autograd/custom_function.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/Dtype.h>
+#include <c10/core/AutogradState.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 
@@ -426,6 +427,13 @@ struct ScanFn : torch::autograd::Function<ScanFn> {
     }
 };
 
+// A tensor with a tangent asks for no gradient: without this it would pass for one that nothing is to be derived from, and the
+// result's missing tangent for zero.
+void no_tangents(std::initializer_list<at::Tensor> ts, const char* where) {
+    if (!c10::AutogradState::get_tls_state().get_fw_grad_mode()) return;
+    for (const at::Tensor& t : ts)
+        TORCH_CHECK_NOT_IMPLEMENTED(!t.defined() || !t._fw_grad(0).defined(), where, ": no forward-mode derivatives (torch.autograd.forward_ad)");
+}
 bool wants_grad(std::initializer_list<at::Tensor> ts) {
     if (!at::GradMode::is_enabled()) return false;
     for (const at::Tensor& t : ts)
@@ -440,6 +448,7 @@ PyObject* gated_scan(PyObject*, PyObject* const* a, Py_ssize_t nargs) {        /
     const int mix = PyObject_IsTrue(a[4]);
     if (mix < 0) throw python_error();
     const int64_t format = integer(a[5], "format");
+    no_tangents({g, x, h0}, "gated_scan");
     dn_status st = DN_OK;
     torch::autograd::variable_list out;
     {
@@ -505,6 +514,7 @@ PyObject* activation(PyObject*, PyObject* const* a, Py_ssize_t nargs) {        /
     HANDLE_TH_ERRORS
     const at::Tensor& x = a_tensor(a[0], "x");
     const int64_t kind = integer(a[1], "kind"), format = integer(a[2], "format");
+    no_tangents({x}, "activation");
     dn_status st = DN_OK;
     at::Tensor y;
     {
