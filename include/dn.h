@@ -285,7 +285,7 @@ const char* dn_kernel_name(const dn_problem* problem, const float* u, const floa
  * intermediate tensors is what bounds the size of the fields ("DiffNets": about 64 GB at 512^2 with 64 samples).  These entry points
  * take fields in 32 or 16 bits; all arithmetic is in 32 bits, each result is rounded once.  Results depend on no order of execution: no
  * atomics.  Where the blocks of a thread-block cluster wait for one another or for a copy, the wait has a limit; should it ever run out,
- * the results behind it are NaN. */
+ * every result of the rows that were waited for and of what depends on them is NaN (what was ahead of them is right). */
 typedef enum { DN_F32 = 0, DN_BF16 = 1, DN_F16 = 2 } dn_type;
 
 /* Values in 8 bits: blocks of 32 share a scale 2^e.  With A the largest finite magnitude of a block, 2^k <= A < 2^(k+1):
@@ -309,11 +309,13 @@ typedef struct {
  * n_b = rows, or lengths[b] (values outside 0 .. rows count as the nearer of the two).  What stands in rows from n_b on, NaN included,
  * plays no part; h, dg and dx are 0 there.  h_last[b] = h_{n_b - 1} (h0[b] if n_b = 0). */
 #define DN_SCAN_MIX 1u
+#define DN_SCAN_GIVE_UP_TILES 0x100u    /* for tests: the waits for a copy, */
+#define DN_SCAN_GIVE_UP_BLOCKS 0x200u   /* for the other blocks of a cluster, give up at once */
 #define DN_SCAN_CHUNK 64         /* rows between two states that a checkpoint keeps in 32 bits */
 typedef struct {
     int32_t batch, rows, cols;   /* batch, cols >= 1, rows >= 0                                             */
     int32_t type;                /* dn_type of g, x, h and their gradients; h0, h_last are 32-bit floats [batch][cols] */
-    uint32_t flags;              /* DN_SCAN_MIX or 0                                                        */
+    uint32_t flags;              /* DN_SCAN_...                                                             */
     int32_t format;              /* dn_format of gate and input in the checkpoint                           */
     const int32_t* lengths;      /* [batch] on the device, or NULL                                          */
 } dn_scan;

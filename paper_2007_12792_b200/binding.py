@@ -31,6 +31,7 @@ DN_F32, DN_BF16, DN_F16 = range(3)
 DN_SAVE_FULL, DN_INT8, DN_E4M3 = range(3)
 DN_SILU, DN_GELU, DN_TANH = range(3)
 DN_SCAN_MIX = 1
+DN_SCAN_GIVE_UP_TILES, DN_SCAN_GIVE_UP_BLOCKS = 0x100, 0x200          # for tests
 DN_SCAN_CHUNK = 64
 FORMATS = {None: DN_SAVE_FULL, "int8": DN_INT8, "e4m3": DN_E4M3}
 ACTIVATIONS = {"silu": DN_SILU, "gelu": DN_GELU, "tanh": DN_TANH}

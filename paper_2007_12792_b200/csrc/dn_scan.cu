@@ -44,6 +44,7 @@ struct ScanArgs {
     int64_t rows_padded;
     int rows, cols, strips, blocks, nblk, nchunk;
     int int8;                    // the input's format (the gate's always is)
+    int copy_tries, block_tries; // limits of the waits for a tile and for the other blocks
 };
 
 template <class T, int V> using Raw = std::conditional_t<sizeof(T) * V == 4, uint32_t, uint16_t>;
@@ -99,11 +100,20 @@ __device__ __forceinline__ void barrier_init(uint64_t* bar) { asm volatile("mbar
 __device__ __forceinline__ void barrier_expect(uint64_t* bar, unsigned bytes) {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"((unsigned)__cvta_generic_to_shared(bar)), "r"(bytes) : "memory");
 }
-// The blocks of a cluster run together, so the wait ends; should it ever not (2^20 tries, each of which suspends the thread for a while),
-// false: the caller's results become NaN.
-__device__ __forceinline__ bool barrier_wait(uint64_t* bar, unsigned parity) {
+// (the condition stands inside: around it the compiler makes two versions of a step, and spills)
+__device__ __forceinline__ void barrier_expect_unless(int lost, uint64_t* bar, unsigned bytes) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.eq.u32 p, %2, 0;\n\t@p mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n\t}" ::"r"((unsigned)__cvta_generic_to_shared(bar)), "r"(bytes),
+                 "r"(lost) : "memory");
+}
+// A copy arrives and the blocks of a cluster run together, so the wait ends; should it ever not (tries: each suspends the thread for
+// about 4 us, a second in all), false.  A thread whose wait ran out is lost: all it finds from then on is NaN, and so is the map of its
+// rows that the others of the block read.  It neither waits again nor sends nor orders anything, so the blocks that would hear from it are
+// lost in turn.
+constexpr int WAIT_TRIES = 1 << 18, LOST = 1 << 20;        // (LOST, what is added to a loop over blocks, is past them all)
+__device__ __forceinline__ bool barrier_wait(uint64_t* bar, unsigned parity, int tries) {
     const unsigned at = (unsigned)__cvta_generic_to_shared(bar);
-    for (int i = 0; i < 1 << 20; ++i) {
+#pragma unroll 1
+    for (int i = 0; i < tries; ++i) {
         unsigned done;
         asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
                      : "=r"(done) : "r"(at), "r"(parity) : "memory");
@@ -131,6 +141,8 @@ __device__ __forceinline__ unsigned char* on_128(unsigned char* shared) {       
     return shared + (-(unsigned)__cvta_generic_to_shared(shared) & 127u);
 }
 __device__ __forceinline__ void shared_to_bulk() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+__device__ __forceinline__ float not_a_number() { return __uint_as_float(0x7fffffffu); }
 
 // factors and offsets of V adjacent columns, in one access
 template <int V> struct __align__(8 * V) Maps { Cols<V> p, h; };
@@ -178,6 +190,7 @@ template <int V, int LX, int WR, int WC, int R> struct Exchange {
     static constexpr int NG = Pl::NG, LANES = WC * LX;
     Maps<V> agg[2][NG > 1 ? NG : 1][NG > 1 ? LANES : 1];
     uint64_t bars[2];
+    int ordered;                 // tiles, where they come by bulk copies
 
     __device__ void init(int K) {
         if (K > 1 && threadIdx.x == 0) {
@@ -189,7 +202,7 @@ template <int V, int LX, int WR, int WC, int R> struct Exchange {
     // The value that enters this thread's rows, from the map (p, h) of these rows and the value `carry` that enters the step's first ones;
     // carry becomes what leaves the last ones.  DOWN: rows are passed from the last to the first.  `between`: what to do once all maps of
     // the block can be read.  sent: what the blocks of the cluster sent, [2][K][LANES].
-    template <bool DOWN, class F> __device__ __forceinline__ Cols<V> enter(Maps<V>* sent, int k, int K, int rank, int q, int lane, const Cols<V>& p, const Cols<V>& h, Cols<V>& carry, bool& lost, F between) {
+    template <bool DOWN, bool TILES, class F> __device__ __forceinline__ Cols<V> enter(Maps<V>* sent, int k, int K, int rank, int q, int lane, const Cols<V>& p, const Cols<V>& h, Cols<V>& carry, int& lost, int tries, F between) {
         if constexpr (NG == 1) {
             const Cols<V> in = carry;
             carry = fma(p, carry, h);
@@ -209,6 +222,7 @@ template <int V, int LX, int WR, int WC, int R> struct Exchange {
                     if (j == q) in = carry;
                     carry = fma(e.p, carry, e.h);
                 }
+                if (TILES && lost) in = all_of<V>(not_a_number());  // (carry is so by this thread's map)
                 return in;
             }
             Cols<V> pb = all_of<V>(1.0f), hb = all_of<V>(0.0f), pt = pb, ht = hb;                // of the groups ahead of this one; of all
@@ -220,12 +234,12 @@ template <int V, int LX, int WR, int WC, int R> struct Exchange {
                 if (i == 0) { pt = e.p; ht = e.h; }
                 else { ht = fma(e.p, ht, e.h); pt = mul(e.p, pt); }
             }
-            for (int peer = q; peer < K; peer += NG) {
+            for (int peer = q + lost; peer < K; peer += NG) {
                 const unsigned to = cluster_address(&sent[(buf * K + rank) * LANES + lane], peer), bar = cluster_address(&bars[buf], peer);
                 if constexpr (V == 1) cluster_send(to, bar, pt.v[0], ht.v[0]); else cluster_send(to, bar, pt.v[0], pt.v[1], ht.v[0], ht.v[1]);
             }
-            if (threadIdx.x == 0) barrier_expect(&bars[buf], K * LANES * (unsigned)sizeof(Maps<V>));
-            lost = lost || !barrier_wait(&bars[buf], (k >> 1) & 1);
+            if (threadIdx.x == 0) barrier_expect_unless(lost, &bars[buf], K * LANES * (unsigned)sizeof(Maps<V>));
+            if (!lost && !barrier_wait(&bars[buf], (k >> 1) & 1, tries)) lost = LOST;
             const int ahead = DOWN ? K - 1 - rank : rank;
 #pragma unroll 4
             for (int i = 0; i < ahead; ++i) {
@@ -238,7 +252,7 @@ template <int V, int LX, int WR, int WC, int R> struct Exchange {
                 const Maps<V> e = sent[(buf * K + (DOWN ? K - 1 - i : i)) * LANES + lane];
                 carry = fma(e.p, carry, e.h);
             }
-            if (lost) in = carry = all_of<V>(__uint_as_float(0x7fffffffu));
+            if (lost) in = carry = all_of<V>(not_a_number());
             return in;
         }
     }
@@ -285,7 +299,7 @@ __global__ void __launch_bounds__(32 * WR * WC, SAVE8 && !BULK ? 3 : 4) scan_for
         }
         __syncthreads();
     }
-    bool lost = false;
+    int lost = 0;
     const float none = S == 4 ? 0.0f : least_decay();
     dep_wait();
     at.read_length(A);
@@ -321,6 +335,7 @@ __global__ void __launch_bounds__(32 * WR * WC, SAVE8 && !BULK ? 3 : 4) scan_for
         }
     };
     [[maybe_unused]] auto order = [&](int s) {             // one thread: the tile of step s
+        ex.ordered = s + 1;
         uint64_t* bar = &tiles.arrived[s % ST];
         unsigned char* to = tiles.in[s % ST];
         const int row = (s * K + at.rank) * TILE;
@@ -329,12 +344,16 @@ __global__ void __launch_bounds__(32 * WR * WC, SAVE8 && !BULK ? 3 : 4) scan_for
         tile_load(to + TILE * ROW, maps.in[1], at.first, row, at.b, bar);
     };
     [[maybe_unused]] auto take = [&](int s) {              // this thread's part of it
-        lost = !barrier_wait(&tiles.arrived[s % ST], (s / ST) & 1) || lost;
+        if (!lost && !barrier_wait(&tiles.arrived[s % ST], (s / ST) & 1, A.copy_tries)) lost = LOST;
         const unsigned char* from = tiles.in[s % ST] + q * R * ROW + at.col * S;
 #pragma unroll
         for (int i = 0; i < R; ++i) {
             rg[i] = *reinterpret_cast<const W*>(from + i * ROW);
             rx[i] = *reinterpret_cast<const W*>(from + TILE * ROW + i * ROW);
+        }
+        if (SAVE8 && lost) {                               // (encode reads such rows from where they come from)
+#pragma unroll
+            for (int i = 0; i < R; ++i) rg[i] = (W)0x7fff7fffu;
         }
     };
     if constexpr (BULK) {
@@ -443,12 +462,13 @@ __global__ void __launch_bounds__(32 * WR * WC, SAVE8 && !BULK ? 3 : 4) scan_for
             __syncwarp();
         }
         if (full) prepare(Yes{}, n); else prepare(No{}, n);
+        if (BULK && lost) P = all_of<V>(not_a_number());
         if constexpr (!BULK)
             if (s + 1 < steps) fetch(row0 + span);         // in flight while the states of this step are found
 
-        Cols<V> hin = ex.template enter<false>(sent, s, K, at.rank, q, at.col / V, P, H, carry, lost, [&] {
+        Cols<V> hin = ex.template enter<false, BULK>(sent, s, K, at.rank, q, at.col / V, P, H, carry, lost, A.block_tries, [&] {
             if constexpr (BULK)
-                if (threadIdx.x == 0 && s + ST < steps) order(s + ST);          // the block has read this step's tile
+                if (threadIdx.x == 0 && !lost && s + ST < steps) order(s + ST);          // the block has read this step's tile
         });
         if (A.states && cv && t0 % kChunkRows == 0 && t0 < A.rows) {
             float* st = A.states + ((int64_t)at.b * A.nchunk + t0 / kChunkRows) * A.cols + c;
@@ -497,7 +517,10 @@ __global__ void __launch_bounds__(32 * WR * WC, SAVE8 && !BULK ? 3 : 4) scan_for
         for (int v = 0; v < V; ++v) A.end[(int64_t)at.b * A.cols + c + v] = carry.v[v];
     }
     if (BULK && (threadIdx.x & 31) == 0) stores_done();
+    if (BULK && lost && threadIdx.x == 0)                  // the block stays until what is on its way to it has landed
+        for (int i = max(ex.ordered - ST, 0); i < ex.ordered; ++i) barrier_wait(&tiles.arrived[i % ST], (i / ST) & 1, WAIT_TRIES);
     if (K > 1) { cluster_arrive(); cluster_wait(); }       // no block's shared memory goes while another could write to it
+    if (lost) __nanosleep(100000);                         // nor while what another sent before it was lost is on its way
 }
 
 // ---- backward ----------------------------------------------------------------------------------------------------------------
@@ -530,7 +553,7 @@ __global__ void __launch_bounds__(32 * WR * WC, 16 / (WR * WC)) scan_backward_ke
         }
         __syncthreads();
     }
-    bool lost = false;
+    int lost = 0;
     const float none = S == 4 ? 0.0f : least_decay();
     dep_wait();
     at.read_length(A);
@@ -597,6 +620,7 @@ __global__ void __launch_bounds__(32 * WR * WC, 16 / (WR * WC)) scan_backward_ke
         if (at.all && r0 + TILE <= len) fetch_rows(Yes{}, r0); else fetch_rows(No{}, r0);
     };
     [[maybe_unused]] auto order = [&](int k) {             // one thread: the tile of the k-th step
+        ex.ordered = k + 1;
         uint64_t* bar = &tiles.arrived[k % ST];
         unsigned char* to = tiles.in[k % ST];
         const int row = ((steps - 1 - k) * K + at.rank) * TILE;
@@ -606,7 +630,7 @@ __global__ void __launch_bounds__(32 * WR * WC, 16 / (WR * WC)) scan_backward_ke
         if (bd) tile_load(to + 2 * TILE * QROW, maps.in[2], at.first, row, at.b, bar);
     };
     [[maybe_unused]] auto take = [&](int k) {              // this thread's part of it
-        lost = !barrier_wait(&tiles.arrived[k % ST], (k / ST) & 1) || lost;
+        if (!lost && !barrier_wait(&tiles.arrived[k % ST], (k / ST) & 1, A.copy_tries)) lost = LOST;
         const unsigned char *from = tiles.in[k % ST] + q * R * QROW + at.col * (QROW / (32 * V)), *fd = tiles.in[k % ST] + 2 * TILE * QROW + q * R * ROW + at.col * S;
 #pragma unroll
         for (int i = 0; i < R; ++i) {
@@ -716,12 +740,13 @@ __global__ void __launch_bounds__(32 * WR * WC, 16 / (WR * WC)) scan_backward_ke
             __syncwarp();
         }
         if (full) prepare(Yes{}, n); else prepare(No{}, n);
+        if (BULK && lost) P = all_of<V>(not_a_number());
         if (s > 0) fetch(row0 - span);                     // (with bulk copies: states and scales)
 
         if constexpr (NG > 1) aggH[buf][q][lane] = H;
-        const Cols<V> mu = ex.template enter<true>(sent, k, K, at.rank, q, lane, P, M, carry, lost, [&] {
+        const Cols<V> mu = ex.template enter<true, BULK>(sent, k, K, at.rank, q, lane, P, M, carry, lost, A.block_tries, [&] {
             if constexpr (BULK)
-                if (threadIdx.x == 0 && k + ST < steps) order(k + ST);          // the block has read this step's tile
+                if (threadIdx.x == 0 && !lost && k + ST < steps) order(k + ST);          // the block has read this step's tile
             if constexpr (NG > 1)
                 for (int j = q - qc; j < q; ++j) hin = fma(ex.agg[buf][j][lane].p, hin, aggH[buf][j][lane]);
         });
@@ -742,7 +767,10 @@ __global__ void __launch_bounds__(32 * WR * WC, 16 / (WR * WC)) scan_backward_ke
         for (int v = 0; v < V; ++v) A.end[(int64_t)at.b * A.cols + c + v] = carry.v[v];
     }
     if (BULK && (threadIdx.x & 31) == 0) stores_done();
+    if (BULK && lost && threadIdx.x == 0)                  // the block stays until what is on its way to it has landed
+        for (int i = max(ex.ordered - ST, 0); i < ex.ordered; ++i) barrier_wait(&tiles.arrived[i % ST], (i / ST) & 1, WAIT_TRIES);
     if (K > 1) { cluster_arrive(); cluster_wait(); }
+    if (lost) __nanosleep(100000);
 }
 
 // ---- launches ----------------------------------------------------------------------------------------------------------------
@@ -756,7 +784,12 @@ struct Shape {                   // of a launch
     int piece;                   // rows that a warp of those stores
     int sent;                    // bytes that a block of a cluster receives per block and step
     double latency;              // us of a step of a block that has its SM to itself
-    int shared(int blocks) const { return (tiles ? tiles + 128 : 0) + (blocks > 1 ? 2 * blocks * sent : 0); }
+    // With bulk copies at least what lets 512 threads onto an SM (of its 228 KB), no more: 32-bit kernels have registers for another
+    // block, and with it 64 x 1024^2 is 228 us backward in place of 218, 16 x 1024^2 from 8 bits 81 in place of 76 (the last wave is emptier).
+    int shared(int blocks) const {
+        const int need = (tiles ? tiles + 128 : 0) + (blocks > 1 ? 2 * blocks * sent : 0), least = tiles ? (228 << 10) / (512 / threads + 1) : 0;
+        return need > least ? need : least;
+    }
 };
 template <int V, int LX, int WR, int WC, int R> Shape shape_of(Kernel k, bool split, int tiles = 0) {
     using Pl = Place<V, LX, WR, WC, R>;
@@ -947,6 +980,8 @@ dn_status launch(const dn_scan& s, bool pairs, bool forward, ScanArgs& A, cudaSt
     if (n * blocks > MOST_GRID) return DN_ERR_SIZE;
     A.strips = (s.cols + f.cols - 1) / f.cols;
     A.blocks = blocks;
+    A.copy_tries = s.flags & DN_SCAN_GIVE_UP_TILES ? 0 : WAIT_TRIES;
+    A.block_tries = s.flags & DN_SCAN_GIVE_UP_BLOCKS ? 0 : WAIT_TRIES;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(n * blocks)); cfg.blockDim = dim3(f.threads); cfg.stream = stream; cfg.dynamicSmemBytes = f.shared(blocks);
     cudaLaunchAttribute attr[2];
@@ -963,7 +998,7 @@ dn_status launch(const dn_scan& s, bool pairs, bool forward, ScanArgs& A, cudaSt
 dn_status check(const dn_scan* s) {
     if (!s) return DN_ERR_NULL;
     if (s->batch < 1 || s->cols < 1 || s->rows < 0 || s->rows > (1 << 30) || s->cols > (1 << 30)) return DN_ERR_SIZE;
-    if (s->type < DN_F32 || s->type > DN_F16 || (s->flags & ~DN_SCAN_MIX) || s->format < DN_SAVE_FULL || s->format > DN_E4M3) return DN_ERR_MODE;
+    if (s->type < DN_F32 || s->type > DN_F16 || (s->flags & ~(DN_SCAN_MIX | DN_SCAN_GIVE_UP_TILES | DN_SCAN_GIVE_UP_BLOCKS)) || s->format < DN_SAVE_FULL || s->format > DN_E4M3) return DN_ERR_MODE;
     // the most rows that a call touches, in elements and bytes, stay far below 2^63
     if ((double)s->batch * s->rows * s->cols > 1e15) return DN_ERR_SIZE;
     if ((((int64_t)s->cols + 7) / 8) * s->batch * SCAN_MOST_BLOCKS > MOST_GRID && (((int64_t)s->cols + 31) / 32) * s->batch * 4 > MOST_GRID) return DN_ERR_SIZE;
