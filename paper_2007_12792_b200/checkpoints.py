@@ -56,9 +56,10 @@ class saved_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
         self._keep, self._places = tuple(keep), frozenset()    # held: an address stands for its tensor only while that lives
 
         def put(t):
+            # kept as it is: without its history, through which an op's saved output would hold the op and so itself, for good
             if not t.is_cuda or t.layout != torch.strided or t.dtype not in TYPES or t.numel() < min_numel:
-                return t
-            return t if t.untyped_storage().data_ptr() in self._places else pack(t, format)
+                return t.detach()
+            return t.detach() if t.untyped_storage().data_ptr() in self._places else pack(t, format)
 
         super().__init__(put, lambda p: p.unpack() if isinstance(p, Packed) else p)
 

@@ -1,0 +1,34 @@
+"""What saved_in_8_bits does with the tensors that it leaves as they are (on the CPU, where these are all tensors)."""
+import gc
+import weakref
+
+import pytest
+import torch
+
+from paper_2007_12792_b200 import checkpoints
+
+
+def test_saved_outputs_are_let_go():
+    """exp saves its result: with a hook that hands it back, result and op would hold one another and never be freed."""
+    x = torch.randn(100, dtype=torch.float64, requires_grad=True)
+    with checkpoints.saved_in_8_bits():
+        y = torch.exp(x)
+        z = (torch.tanh(y) * y).sum()
+    gone = [weakref.ref(y), weakref.ref(z)]
+    del y, z
+    gc.collect()
+    assert [r() for r in gone] == [None, None]
+
+
+def test_gradients_of_what_is_kept():
+    """First and second derivatives are those without the context."""
+    x = torch.linspace(-1.0, 1.0, 50, dtype=torch.float64).requires_grad_()
+    w = torch.randn(50, dtype=torch.float64, generator=torch.Generator().manual_seed(1)).requires_grad_()
+    out = []
+    for context in (checkpoints.saved_in_8_bits(keep=[w]), torch.enable_grad()):
+        with context:
+            y = (torch.exp(w * x) * torch.sigmoid(x)).sum()
+            g = torch.autograd.grad(y, (x, w), create_graph=True)
+            out.append([*g, *torch.autograd.grad((g[0] ** 2).sum() + g[1].sum(), (x, w))])
+    for a, b in zip(*out):
+        assert torch.equal(a, b)
