@@ -40,6 +40,20 @@ def pack(x: torch.Tensor, format: str = "int8") -> Packed:
     return Packed(data, format, x.shape, x.dtype)
 
 
+class _Kept:
+    """A saved tensor as it is: without its history, through which an op's saved output would hold the op and so itself, for good;
+    with its version, which autograd looks at only where no hooks are."""
+
+    def __init__(self, t: torch.Tensor):
+        self.tensor, self.version = t.detach(), t._version
+
+    def unpack(self) -> torch.Tensor:
+        if self.tensor._version != self.version:
+            raise RuntimeError(f"a saved tensor of shape {list(self.tensor.shape)}, kept as it is, has been modified in place: "
+                               f"version {self.tensor._version} in place of {self.version}")
+        return self.tensor
+
+
 class saved_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
     """Context in which the floating-point CUDA tensors that autograd saves are kept in 8 bits:
 
@@ -48,7 +62,8 @@ class saved_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
         loss.backward()
 
     keep: tensors that stay as they are, views of them too (weights, which the gradient of the input multiplies with); so do
-    tensors of less than ``min_numel`` elements.  A gradient is then that of the ops at the values which 8 bits hold.  A tensor that
+    tensors of less than ``min_numel`` elements.  They must not change before the backward pass, which raises RuntimeError if they
+    have (an optimiser's step in between, say).  A gradient is then that of the ops at the values which 8 bits hold.  A tensor that
     several ops save is kept once for each of them."""
 
     def __init__(self, format: str = "int8", keep: Iterable[torch.Tensor] = (), min_numel: int = 4096):
@@ -56,12 +71,11 @@ class saved_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
         self._keep, self._places = tuple(keep), frozenset()    # held: an address stands for its tensor only while that lives
 
         def put(t):
-            # kept as it is: without its history, through which an op's saved output would hold the op and so itself, for good
             if not t.is_cuda or t.layout != torch.strided or t.dtype not in TYPES or t.numel() < min_numel:
-                return t.detach()
-            return t.detach() if t.untyped_storage().data_ptr() in self._places else pack(t, format)
+                return _Kept(t)
+            return _Kept(t) if t.untyped_storage().data_ptr() in self._places else pack(t, format)
 
-        super().__init__(put, lambda p: p.unpack() if isinstance(p, Packed) else p)
+        super().__init__(put, lambda p: p.unpack())
 
     def __enter__(self):
         self._places = frozenset(k.untyped_storage().data_ptr() for k in self._keep if k.is_cuda)

@@ -32,3 +32,32 @@ def test_gradients_of_what_is_kept():
             out.append([*g, *torch.autograd.grad((g[0] ** 2).sum() + g[1].sum(), (x, w))])
     for a, b in zip(*out):
         assert torch.equal(a, b)
+
+
+def test_what_is_kept_must_not_change():
+    """A weight updated between forward and backward pass, or any kept tensor written into: an error, as without the context."""
+    for change in (lambda w, v: w.add_(1.0), lambda w, v: v.zero_()):
+        w, x = torch.randn(5000, requires_grad=True), torch.randn(5000, requires_grad=True)
+        v = torch.randn(5000)
+        with checkpoints.saved_in_8_bits(keep=[w]):
+            y = (w * x * v).sum()
+        with torch.no_grad():
+            change(w, v)
+        with pytest.raises(RuntimeError, match="modified in place"):
+            torch.autograd.grad(y, (w, x))
+
+
+@pytest.mark.gpu
+def test_what_is_kept_on_the_device_must_not_change():
+    w, x = torch.randn(5000, device="cuda", requires_grad=True), torch.randn(5000, device="cuda", requires_grad=True)
+    for keep in ([w], ()):
+        with checkpoints.saved_in_8_bits(keep=keep):
+            y = (w.view(50, 100) * x.view(50, 100)).sum()
+        want = checkpoints.pack(w.detach()).unpack()
+        with torch.no_grad():
+            w.add_(1.0)
+        if keep:
+            with pytest.raises(RuntimeError, match="modified in place"):
+                torch.autograd.grad(y, x)
+        else:                                            # 8 bits hold a copy
+            assert torch.equal(torch.autograd.grad(y, x)[0], want)
