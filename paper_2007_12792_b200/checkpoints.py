@@ -62,7 +62,7 @@ class saved_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
         loss.backward()
 
     keep: tensors that stay as they are, views of them too (weights, which the gradient of the input multiplies with); so do
-    tensors of less than ``min_numel`` elements.  They must not change before the backward pass, which raises RuntimeError if they
+    tensors of less than ``min_numel`` elements, and expanded views whose memory is no more than 8 bits for each element.  They must not change before the backward pass, which raises RuntimeError if they
     have (an optimiser's step in between, say).  A gradient is then that of the ops at the values which 8 bits hold.  A tensor that
     several ops save is kept once for each of them."""
 
@@ -73,7 +73,10 @@ class saved_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
         def put(t):
             if not t.is_cuda or t.layout != torch.strided or t.dtype not in TYPES or t.numel() < min_numel:
                 return _Kept(t)
-            return _Kept(t) if t.untyped_storage().data_ptr() in self._places else pack(t, format)
+            memory = t.untyped_storage()                   # of an expanded view: less than its elements
+            if memory.data_ptr() in self._places or memory.nbytes() <= t.numel() + t.numel() // 32:
+                return _Kept(t)
+            return pack(t, format)
 
         super().__init__(put, lambda p: p.unpack())
 

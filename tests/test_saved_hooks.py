@@ -61,3 +61,25 @@ def test_what_is_kept_on_the_device_must_not_change():
                 torch.autograd.grad(y, x)
         else:                                            # 8 bits hold a copy
             assert torch.equal(torch.autograd.grad(y, x)[0], want)
+
+
+@pytest.mark.gpu
+def test_expanded_views_take_no_more_memory():
+    """A row that all rows share is 4 kB; a byte for each element of the view would be 8 MB."""
+    row, x = torch.randn(1024, device="cuda"), torch.randn(8192, 1024, device="cuda", requires_grad=True)
+    torch.cuda.synchronize()
+    start = torch.cuda.memory_allocated()
+    with checkpoints.saved_in_8_bits():
+        y = x * row.expand(8192, 1024)
+    del y
+    with checkpoints.saved_in_8_bits():
+        y = x * row.expand(8192, 1024)
+        assert torch.cuda.memory_allocated() - start <= 4 * x.numel() + (1 << 20)           # the result alone (x wants a gradient, the row none)
+    d = torch.randn_like(x)
+    assert torch.equal(torch.autograd.grad(y, x, d)[0], d * row)
+    # a view that is expanded a little is smaller in 8 bits
+    half = torch.randn(8192, 512, device="cuda")
+    with checkpoints.saved_in_8_bits():
+        z = x.view(8192, 2, 512) * half[:, None].expand(8192, 2, 512)
+    packed = checkpoints.pack(half[:, None].expand(8192, 2, 512)).unpack().view(8192, 1024)
+    assert torch.equal(torch.autograd.grad(z.view(8192, 1024), x, d)[0], d * packed)
