@@ -12,6 +12,7 @@ from typing import Optional, Tuple
 import torch
 
 from . import binding as B
+from . import checkpoints
 
 
 def _apply(name, where, function, u, problem, workspace):
@@ -81,7 +82,12 @@ def gated_scan(gate: torch.Tensor, x: torch.Tensor, h0: Optional[torch.Tensor] =
 
     checkpoint None keeps gate, x and the state ahead of every 64th row for the backward pass; "int8" or "e4m3" keeps gate and x
     in 8 bits instead (the gate as int8 in either), and the gradients are those at the values that 8 bits hold."""
-    out = B.native().gated_scan(gate, x, h0, lengths, mix, B._format(checkpoint, none=True))
+    kept = B._format(checkpoint, none=True)
+    checkpoints.saving.gate = checkpoint is None
+    try:
+        out = B.native().gated_scan(gate, x, h0, lengths, mix, kept)
+    finally:
+        checkpoints.saving.gate = False
     if isinstance(out, int):
         raise B.DnError(out, "dn_scan_forward")
     return out

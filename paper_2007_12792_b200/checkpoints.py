@@ -6,6 +6,7 @@ that is a power of two ("int8": errors of at most 1/128 of the block's largest m
 a value that is not finite comes back as NaN."""
 from __future__ import annotations
 
+import threading
 from dataclasses import dataclass
 from typing import Iterable
 
@@ -40,6 +41,15 @@ def pack(x: torch.Tensor, format: str = "int8") -> Packed:
     return Packed(data, format, x.shape, x.dtype)
 
 
+class _Saving(threading.local):
+    """Set by gated_scan while it saves: the first tensor of numbers is its gate, which 8 bits hold as int8 in either format (an e4m3
+    number is off relative to itself, and what counts of a gate of 7 is one minus its sigmoid)."""
+    gate = False
+
+
+saving = _Saving()
+
+
 class _Kept:
     """A saved tensor as it is: without its history, through which an op's saved output would hold the op and so itself, for good;
     with its version, which autograd looks at only where no hooks are."""
@@ -64,19 +74,22 @@ class saved_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
     keep: tensors that stay as they are, views of them too (weights, which the gradient of the input multiplies with); so do
     tensors of less than ``min_numel`` elements, and expanded views whose memory is no more than 8 bits for each element.  They must not change before the backward pass, which raises RuntimeError if they
     have (an optimiser's step in between, say).  A gradient is then that of the ops at the values which 8 bits hold.  A tensor that
-    several ops save is kept once for each of them."""
+    several ops save is kept once for each of them.  The gate of ``autograd.gated_scan`` is kept as int8 in either format."""
 
     def __init__(self, format: str = "int8", keep: Iterable[torch.Tensor] = (), min_numel: int = 4096):
         B._format(format)
         self._keep, self._places = tuple(keep), frozenset()    # held: an address stands for its tensor only while that lives
 
         def put(t):
+            gate = saving.gate and t.is_floating_point()
+            if gate:
+                saving.gate = False
             if not t.is_cuda or t.layout != torch.strided or t.dtype not in TYPES or t.numel() < min_numel:
                 return _Kept(t)
             memory = t.untyped_storage()                   # of an expanded view: less than its elements
             if memory.data_ptr() in self._places or memory.nbytes() <= t.numel() + t.numel() // 32:
                 return _Kept(t)
-            return pack(t, format)
+            return pack(t, "int8" if gate else format)
 
         super().__init__(put, lambda p: p.unpack())
 

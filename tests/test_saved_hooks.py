@@ -5,7 +5,8 @@ import weakref
 import pytest
 import torch
 
-from paper_2007_12792_b200 import checkpoints
+import scan_util as S
+from paper_2007_12792_b200 import autograd, checkpoints
 
 
 def test_saved_outputs_are_let_go():
@@ -83,3 +84,26 @@ def test_expanded_views_take_no_more_memory():
         z = x.view(8192, 2, 512) * half[:, None].expand(8192, 2, 512)
     packed = checkpoints.pack(half[:, None].expand(8192, 2, 512)).unpack().view(8192, 1024)
     assert torch.equal(torch.autograd.grad(z.view(8192, 1024), x, d)[0], d * packed)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_a_gate_is_kept_as_int8(dtype):
+    """gated_scan inside the context (rows of 64 columns: the blocks of 32 are those of its own checkpoint): the gradients at the gate in
+    int8 and the input in the context's format, also where a gate of 12 would be off by half a unit in e4m3."""
+    g, x, gen = S.fields(2, 130, 64, dtype, 5, gate=(-1.0, 12.0))
+    leaves = [g.requires_grad_(), x.requires_grad_()]
+    d = torch.randn(2, 130, 64, device="cuda", generator=gen).to(dtype)
+    for fmt in ("e4m3", "int8"):
+        with checkpoints.saved_in_8_bits(fmt):
+            h, _ = autograd.gated_scan(*leaves, mix=True)
+            y = torch.exp(x)                             # what is saved next is no gate
+        dg, dx = torch.autograd.grad(h, leaves, d)
+        wg, wx, _, eg, ex, _ = S.backward(g.detach(), x.detach(), None, None, True, d, None, fmt)
+        S.check(dg, wg, eg, dtype, "dg")
+        S.check(dx, wx, ex, dtype, "dx")
+        assert torch.equal(torch.autograd.grad(y, x, d)[0], d * checkpoints.pack(y.detach(), fmt).unpack())
+    h, _ = autograd.gated_scan(*leaves)                  # outside: nothing is left over for the context after it
+    with checkpoints.saved_in_8_bits("e4m3"):
+        y = torch.exp(x)
+    assert torch.equal(torch.autograd.grad(y, x, d)[0], d * checkpoints.pack(y.detach(), "e4m3").unpack())
