@@ -323,7 +323,8 @@ typedef struct {
 /* Bytes of the checkpoint that dn_scan_forward leaves for dn_scan_backward: the state ahead of every 64th row in 32 bits; with
  * DN_INT8 or DN_E4M3 also gate and input in 8 bits, so that neither g nor x has to be kept (2.1 bytes per element in place of 4 or
  * 8).  The gate is kept as DN_INT8 in either format: its error has to be small next to 1, not next to itself, or slow decays
- * (1 - a = exp(-g) for large g) are lost.  0 if the call is invalid. */
+ * (1 - a = exp(-g) for large g) are lost; and held to +-63.5, where a and 1 - a are 0 or 1 to 2^-91: so infinite gates have a code, and the
+ * gates of the 32 columns around one of -1e4, say, still have steps of 1/2.  0 if the call is invalid. */
 size_t dn_scan_checkpoint_bytes(const dn_scan* scan);
 
 /* h and h_last.  checkpoint (256-byte aligned, or NULL: nothing is kept) belongs to the caller, who hands it to the backward call.

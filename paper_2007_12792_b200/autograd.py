@@ -81,7 +81,7 @@ def gated_scan(gate: torch.Tensor, x: torch.Tensor, h0: Optional[torch.Tensor] =
     gate and x: CUDA tensors of one type (float32, bfloat16, float16).  Differentiable once, backward, with respect to gate, x and h0.
 
     checkpoint None keeps gate, x and the state ahead of every 64th row for the backward pass; "int8" or "e4m3" keeps gate and x
-    in 8 bits instead (the gate as int8 in either), and the gradients are those at the values that 8 bits hold."""
+    in 8 bits instead (the gate as int8 in either, held to +-63.5), and the gradients are those at the values that 8 bits hold."""
     kept = B._format(checkpoint, none=True)
     checkpoints.saving.gate = checkpoint is None
     try:

@@ -43,7 +43,8 @@ def pack(x: torch.Tensor, format: str = "int8") -> Packed:
 
 class _Saving(threading.local):
     """Set by gated_scan while it saves: the first tensor of numbers is its gate, which 8 bits hold as int8 in either format (an e4m3
-    number is off relative to itself, and what counts of a gate of 7 is one minus its sigmoid)."""
+    number is off relative to itself, and what counts of a gate of 7 is one minus its sigmoid), within +-63.5 (the sigmoid is 0 or 1
+    to 2^-91 there; a mask of -1e4 would leave its neighbours steps of 64)."""
     gate = False
 
 
@@ -74,7 +75,8 @@ class saved_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
     keep: tensors that stay as they are, views of them too (weights, which the gradient of the input multiplies with); so do
     tensors of less than ``min_numel`` elements, and expanded views whose memory is no more than 8 bits for each element.  They must not change before the backward pass, which raises RuntimeError if they
     have (an optimiser's step in between, say).  A gradient is then that of the ops at the values which 8 bits hold.  A tensor that
-    several ops save is kept once for each of them.  The gate of ``autograd.gated_scan`` is kept as int8 in either format."""
+    several ops save is kept once for each of them.  The gate of ``autograd.gated_scan`` is kept as int8 in either format,
+    held to +-63.5."""
 
     def __init__(self, format: str = "int8", keep: Iterable[torch.Tensor] = (), min_numel: int = 4096):
         B._format(format)
@@ -89,7 +91,7 @@ class saved_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
             memory = t.untyped_storage()                   # of an expanded view: less than its elements
             if memory.data_ptr() in self._places or memory.nbytes() <= t.numel() + t.numel() // 32:
                 return _Kept(t)
-            return pack(t, "int8" if gate else format)
+            return pack(t.detach().clamp(-63.5, 63.5), "int8") if gate else pack(t, format)
 
         super().__init__(put, lambda p: p.unpack())
 

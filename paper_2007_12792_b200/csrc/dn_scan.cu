@@ -79,6 +79,22 @@ template <class T, int V> __device__ __forceinline__ void gate_parts(Raw<T, V> r
     else if constexpr (V == 2) gates<false, true>(expand<T, V>(held(r, T())), a, w, none);
     else gates<false>(expand<T, V>(r), a, w, none);
 }
+// The gate of an 8-bit checkpoint is held to +-63.5 = 127 / 2, where its sigmoid is 1 or 0 to 2^-91: its 32 neighbours have steps of 1/2 at
+// most, and an infinite one has a code.  Its bits without the sign, of 32-bit values the upper 16:
+template <class T> inline constexpr uint32_t MOST_GATE8 = std::is_same_v<T, __half> ? 0x53f0u : 0x427eu;
+__device__ __forceinline__ uint32_t held8(uint32_t r, __nv_bfloat16) {
+    asm("min.NaN.bf16x2 %0, %0, %1;\n\tmax.NaN.bf16x2 %0, %0, %2;" : "+r"(r) : "r"(0x427e427eu), "r"(0xc27ec27eu));
+    return r;
+}
+__device__ __forceinline__ uint32_t held8(uint32_t r, __half) {
+    asm("min.NaN.f16x2 %0, %0, %1;\n\tmax.NaN.f16x2 %0, %0, %2;" : "+r"(r) : "r"(0x53f053f0u), "r"(0xd3f0d3f0u));
+    return r;
+}
+__device__ __forceinline__ uint32_t held8(uint32_t r, float) { return r; }               // (not needed)
+__device__ __forceinline__ float held8(float v) {
+    asm("min.NaN.f32 %0, %0, %1;\n\tmax.NaN.f32 %0, %0, %2;" : "+f"(v) : "f"(63.5f), "f"(-63.5f));
+    return v;
+}
 template <class W> __device__ __forceinline__ W load_at(const char* p) { return *reinterpret_cast<const W*>(p); }
 template <class W> __device__ __forceinline__ void store_at(char* p, W v) { *reinterpret_cast<W*>(p) = v; }
 
@@ -405,10 +421,10 @@ __global__ void __launch_bounds__(32 * WR * WC, SAVE8 && !BULK ? 3 : 4) scan_for
             const char *g = bg + row0 * A.g.row, *x = bx + row0 * A.x.row;
 #pragma unroll 1
             for (int i = 0; i < R; ++i) {
-                const Cols<V> vg = expand<T, V>(i < n ? load_at<W>(g + i * A.g.row + og) : W(0)), vx = expand<T, V>(i < n ? load_at<W>(x + i * A.x.row + ox) : W(0));
+                Cols<V> vg = expand<T, V>(i < n ? load_at<W>(g + i * A.g.row + og) : W(0)), vx = expand<T, V>(i < n ? load_at<W>(x + i * A.x.row + ox) : W(0));
                 unsigned mg = 0, mx = 0;
 #pragma unroll
-                for (int v = 0; v < V; ++v) { mg = max(mg, magnitude_bits(vg.v[v])); mx = max(mx, magnitude_bits(vx.v[v])); }
+                for (int v = 0; v < V; ++v) { vg.v[v] = held8(vg.v[v]); mg = max(mg, magnitude_bits(vg.v[v])); mx = max(mx, magnitude_bits(vx.v[v])); }
 #pragma unroll
                 for (int h = V == 2 ? 8 : 16; h >= 1; h /= 2) { mg = max(mg, __shfl_xor_sync(~0u, mg, h)); mx = max(mx, __shfl_xor_sync(~0u, mx, h)); }
                 const int sg = scale_byte(mg, true), sx = scale_byte(mx, A.int8);
@@ -423,17 +439,26 @@ __global__ void __launch_bounds__(32 * WR * WC, SAVE8 && !BULK ? 3 : 4) scan_for
             }
             return;
         }
-        const int sg = max(eg - 6, 1), sx = max(exx - (A.int8 ? 6 : 7), 1);
+        const int sg = max(min(eg, 132) - 6, 1), sx = max(exx - (A.int8 ? 6 : 7), 1);
         if (mine && (V == 2 || lane < 16)) { gs[lane & 15] = (uint8_t)sg; xs[lane & 15] = (uint8_t)sx; }
         const uint32_t inverse = (uint32_t)(254 - sg) << 7 | (uint32_t)(254 - sx) << 23;            // upper halves of the two floats
+        auto codes = [&](auto far) {
 #pragma unroll
-        for (int i = 0; i < R; ++i) {
-            const uint32_t both = __shfl_sync(~0u, inverse, V == 2 ? (lane & 16) | i : i);
-            const uint32_t kg = codes_int8(expand<T, V>(rg[i]), __uint_as_float(both << 16));
-            const Cols<V> vx = expand<T, V>(rx[i]);
-            const float ix = __uint_as_float(both & 0xffff0000u);
-            put(i, kg, A.int8 ? codes_int8(vx, ix) : codes_e4m3(vx, ix));
+            for (int i = 0; i < R; ++i) {
+                const uint32_t both = __shfl_sync(~0u, inverse, V == 2 ? (lane & 16) | i : i);
+                W g = rg[i];
+                if constexpr (decltype(far)::value) g = (W)held8(g, T());
+                const uint32_t kg = codes_int8(expand<T, V>(g), __uint_as_float(both << 16));
+                const Cols<V> vx = expand<T, V>(rx[i]);
+                const float ix = __uint_as_float(both & 0xffff0000u);
+                put(i, kg, A.int8 ? codes_int8(vx, ix) : codes_e4m3(vx, ix));
+            }
+        };
+        // (codes of single values are held to 127 themselves)
+        if constexpr (V == 2) {
+            if (__any_sync(~0u, (m[0] & 0xffffu) > MOST_GATE8<T>)) { codes(Yes{}); return; }
         }
+        codes(No{});
     };
 
     Cols<V> a[R], bb[R], P, H;
