@@ -307,7 +307,11 @@ typedef struct {
  *   h_t = a_t h_{t-1} + w_t x_t,   t = 0 .. n_b - 1,   h_{-1} = h0 (0 where h0 is NULL)
  *
  * n_b = rows, or lengths[b] (values outside 0 .. rows count as the nearer of the two).  What stands in rows from n_b on, NaN included,
- * plays no part; h, dg and dx are 0 there.  h_last[b] = h_{n_b - 1} (h0[b] if n_b = 0). */
+ * plays no part; h, dg and dx are 0 there.  h_last[b] = h_{n_b - 1} (h0[b] if n_b = 0).
+ *
+ * a_t is a 32-bit number, off by up to 2^-25 with 32-bit fields and 2^-23 with 16-bit ones: what n rows of slow decay have passed on is off by
+ * up to n times that of itself (and n 2^-23 of rounding), in h_last, dh0 and the states kept too, which are 32-bit results for every type.  From
+ * g = 17 or 18 up a_t is 1. */
 #define DN_SCAN_MIX 1u
 #define DN_SCAN_GIVE_UP_TILES 0x100u    /* for tests: the waits for a copy, */
 #define DN_SCAN_GIVE_UP_BLOCKS 0x200u   /* for the other blocks of a cluster, give up at once */

@@ -109,6 +109,8 @@ template <bool ACCURATE> __device__ __forceinline__ void two_sided_gates(float z
 
 // The same as the decay and the input's weight of the recurrence.  For 16-bit types with z held to at least LEAST_GATE, so that e^-z cannot
 // overflow, and what that leaves of p (2^-125) taken away, so that p is 0 there: 6 operations instead of some 16, 10 for two columns.
+// Of p near 1 that is off by 2^-23 at most (1 + e^-z rounded, its reciprocal an ulp off), 3.5e-8 on average against 1.7e-8 for one minus the
+// smaller part, which would take 5 more operations for two columns; neither keeps more than a few digits of 1 - p where p decays slowly.
 // HELD: the caller has held z.  none: least_decay().
 constexpr float LEAST_GATE = -87.0f;
 __device__ __forceinline__ void exponential_gate(float t, float& e) { asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(t)); }
