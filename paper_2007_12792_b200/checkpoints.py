@@ -2,8 +2,8 @@
 
 ``pack`` puts one tensor into 8 bits, ``saved_in_8_bits`` does so with what the ops inside it save for their backward pass: a
 generator's layers, and the gradient that the losses of ``autograd`` compute with their value.  Blocks of 32 values share a scale
-that is a power of two ("int8": errors of at most 1/128 of the block's largest magnitude, "e4m3": of 1/16 of the value itself);
-a value that is not finite comes back as NaN."""
+that is a power of two ("int8": errors of at most 1/128 of the block's largest magnitude, 1/64 next to it; "e4m3": of 1/16 of the value
+itself, or 2^-17 of the block's largest where that is more: a small value may come back as 0); a value that is not finite comes back as NaN."""
 from __future__ import annotations
 
 import threading
