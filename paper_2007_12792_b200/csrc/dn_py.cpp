@@ -249,14 +249,13 @@ void bytes_checked(const at::Tensor& t, const char* name, Device& d) {
     d.see(t, name);
     TORCH_CHECK_VALUE(t.scalar_type() == at::kByte && t.is_contiguous(), name, ": expected a contiguous uint8 tensor");
 }
-int64_t integer(PyObject* o, const char* name) {
+int64_t integer(PyObject* o) {
     const int64_t v = PyLong_AsLongLong(o);
     if (v == -1 && PyErr_Occurred()) throw python_error();
-    (void)name;
     return v;
 }
 int32_t small_integer(PyObject* o, const char* name) {
-    const int64_t v = integer(o, name);
+    const int64_t v = integer(o);
     TORCH_CHECK_VALUE(v >= INT32_MIN && v <= INT32_MAX, name, ": ", v, " is out of range");
     return (int32_t)v;
 }
@@ -447,7 +446,7 @@ PyObject* gated_scan(PyObject*, PyObject* const* a, Py_ssize_t nargs) {        /
     const at::Tensor &g = a_tensor(a[0], "gate"), &x = a_tensor(a[1], "x"), &h0 = maybe_tensor(a[2], "h0"), &lengths = maybe_tensor(a[3], "lengths");
     const int mix = PyObject_IsTrue(a[4]);
     if (mix < 0) throw python_error();
-    const int64_t format = integer(a[5], "format");
+    const int64_t format = integer(a[5]);
     no_tangents({g, x, h0}, "gated_scan");
     dn_status st = DN_OK;
     torch::autograd::variable_list out;
@@ -513,7 +512,7 @@ PyObject* activation(PyObject*, PyObject* const* a, Py_ssize_t nargs) {        /
     DN_ARGS(3);
     HANDLE_TH_ERRORS
     const at::Tensor& x = a_tensor(a[0], "x");
-    const int64_t kind = integer(a[1], "kind"), format = integer(a[2], "format");
+    const int64_t kind = integer(a[1]), format = integer(a[2]);
     no_tangents({x}, "activation");
     dn_status st = DN_OK;
     at::Tensor y;
@@ -587,7 +586,7 @@ PyObject* unpacked(PyObject*, PyObject* const* a, Py_ssize_t nargs) {          /
     const int32_t format = small_integer(a[1], "format");
     TORCH_CHECK_TYPE(PyTuple_Check(a[2]) && THPDtype_Check(a[3]), "unpack: expected a shape and a dtype");
     std::vector<int64_t> shape;
-    for (Py_ssize_t i = 0; i < PyTuple_GET_SIZE(a[2]); ++i) shape.push_back(integer(PyTuple_GET_ITEM(a[2], i), "shape"));
+    for (Py_ssize_t i = 0; i < PyTuple_GET_SIZE(a[2]); ++i) shape.push_back(integer(PyTuple_GET_ITEM(a[2], i)));
     const at::ScalarType dtype = reinterpret_cast<THPDtype*>(a[3])->scalar_type;
     const int32_t type = type_code(dtype, "dtype");
     Device d;
