@@ -5,8 +5,13 @@
 // forward kernel writes y and the packed input from one read of x; its backward kernel reads the packed input and dy and writes dx: 10 bytes
 // per element of a 16-bit type for both, 12 with the input kept as it is.
 //
-// What bounds them: memory in 32 bits (2^25 values: packing 27 us = 95 % of the measured copy rate, reading back 29 us = 90 %, silu
-// 48 + 49 us = 96 %); in 16 bits the arithmetic per byte shows (packing 21 us = 73 %, silu 31 us = 84 % and 36 us = 71 %, gelu 35 and 45 us).
+// What bounds them: memory in 32 bits (2^25 values: packing 27 us = 95 % of the measured copy rate, reading back 28 us = 91 %, silu and tanh
+// 48 + 48 us = 96 %, gelu 48 + 52 us = 97 and 88 %).  In 16 bits the instructions show (how many per
+// value, and in how many of the cycles a scheduler issued one):
+//   packing  22 us = 72 %   13 instructions, 64 %      reading back  18 us = 84 %    9, 62 %
+//   silu     31 us = 84 %   21, 75 %                   backward      36 us = 72 %   20, 61 % (42 warps per SM, 40 registers)
+//   gelu     35 us = 74 %   26, 78 %                   backward      44 us = 58 %   27, 64 % (36 warps, 44 registers)
+//   tanh     38 us = 68 %   31, 81 % (tanhf)           backward      38 us = 68 %   26, 74 %
 // Measured: four units per thread are slower backward (44 us: fewer warps fit), 16-byte stores of 32-bit values 37 us for 29 (every
 // sector in two halves), streaming hints on loads and stores no gain.
 #include "dn_eight.cuh"

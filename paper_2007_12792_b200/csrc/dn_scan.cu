@@ -12,15 +12,15 @@
 //
 // What moves the data.  Arrays on 16-byte places and strides: tiles of 64 rows (128 rows of half the columns) by bulk copies, two stages
 // ahead of the arithmetic, results back the same way from a piece of shared memory per warp; that takes the address arithmetic off the
-// threads (19 instructions per element of a 16-bit type forward, 29 with plain loads, 35 backward) and the raw tiles off their registers.
-// Others: loads into registers a step ahead.  Rows of few columns: lanes 8 across, 4 groups of rows down.  Up to 16 rows (backward 8):
-// a thread per column, nothing to exchange.
+// threads (18 instructions per element of a 16-bit type forward, 29 with plain loads, 35 backward) and the raw tiles off their registers.
+// Others: loads into registers a step ahead.  Where even clusters of 16 blocks leave SMs idle (fewer strips of columns on the whole device
+// than a sixteenth of its SMs): lanes 8 across, 4 groups of rows down.  Up to 16 rows (backward 8): a thread per column, nothing to exchange.
 //
-// What bounds it.  Memory, where there are strips of columns enough: 1024^2 x 64 in 32 bits 135 us forward (92 % of the measured copy rate)
+// What bounds it.  Memory, where there are strips of columns enough: 1024^2 x 64 in 32 bits 134 us forward (92 % of the measured copy rate)
 // and 218 us backward (95 %), 32 x 2048 x 2048 bf16 139 us (89 %).  With fewer, the last and uneven wave and the latency of a step (about 1 us
-// forward, 1.3 backward: copy, 16 or 8 rows of dependent products, exchange): 8 x 2048 x 2048 bf16 38 us (80 %) and 66 us (78 %), one sequence of
-// 65536 x 2048 167 us (74 %) and 335 us (62 %).  3.1 to 3.4 warps per scheduler fit, limited by the registers that hold a tile, and an
-// instruction is issued in 53 to 55 % of the cycles; most stalls are waits for the result before.
+// forward, 1.3 backward: copy, 16 or 8 rows of dependent products, exchange): 8 x 2048 x 2048 bf16 39 us (80 %) and 66 us (78 %), one sequence of
+// 65536 x 2048 170 us (73 %) and 330 us (63 %).  3.1 to 3.4 warps per scheduler fit, limited by the registers that hold a tile, and an
+// instruction is issued in 54 to 55 % of the cycles; most stalls are waits for the result before.
 // Measured and not kept: five blocks per SM forward (96 registers, a few spilled: 38 -> 44 us); three backward, with x and dh read again
 // from shared memory (66 -> 90 us) or spilled (8-bit checkpoint 147 -> 204 us); dh kept in 16 bits until it is used (66 -> 71 us).
 #include "dn_eight.cuh"
@@ -381,8 +381,8 @@ __global__ void __launch_bounds__(32 * WR * WC, SAVE8 && !BULK ? 3 : 4) scan_for
     [[maybe_unused]] unsigned char* const mine_codes =
         BULK ? tiles.out[threadIdx.x >> 5] + PIECE * ROW + (threadIdx.x & 31) / LX * R * LX * V + at.col : nullptr;
 
-    // (8 x 4096 x 2048 bf16 with its 8-bit checkpoint: 130 us, 64 % of the copy rate, against 310 us with a reduction per row and conversions
-    // by the unit that the exponentials use; 36 instructions per element.)
+    // (8 x 4096 x 2048 bf16 with its 8-bit checkpoint: 133 us, 63 % of the copy rate, against 310 us with a reduction per row and conversions
+    // by the unit that the exponentials use; 38 instructions per element.)
     // Codes and scales of this warp's 16 rows.  The largest magnitudes of the 16 rows are found together: at every stage of a butterfly a lane
     // hands half of its rows to the other and keeps the other's share of the rest, 15 exchanges of gate and input at once in place of 64
     // or 80; lane r then holds row r, works out its scales, and hands them round.
