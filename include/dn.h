@@ -285,7 +285,7 @@ const char* dn_kernel_name(const dn_problem* problem, const float* u, const floa
  * intermediate tensors is what bounds the size of the fields ("DiffNets": about 64 GB at 512^2 with 64 samples).  These entry points
  * take fields in 32 or 16 bits; all arithmetic is in 32 bits, each result is rounded once.  Results depend on no order of execution: no
  * atomics.  Where the blocks of a thread-block cluster wait for one another or for a copy, the wait has a limit; should it ever run out,
- * every result of the rows that were waited for and of what depends on them is NaN (what was ahead of them is right). */
+ * every result that depends on what was waited for is NaN, and others of the same columns and sample may be. */
 typedef enum { DN_F32 = 0, DN_BF16 = 1, DN_F16 = 2 } dn_type;
 
 /* Values in 8 bits: blocks of 32 share a scale 2^e.  With A the largest finite magnitude of a block, 2^k <= A < 2^(k+1):
